@@ -336,6 +336,146 @@ dart_status dart_gated_rmsnorm_bwd(int64_t rows, int32_t dim, int32_t group, int
                                    float* dz, int64_t dz_row_stride, float* dweight,
                                    void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The steps of a language model around its blocks, as training and scoring
+ * run them: the norm of the residual stream, the log probabilities over the
+ * vocabulary, the clipping of the gradients.  rows = 0 (and a list of no
+ * tensors) is allowed: nothing is launched but what writes a defined result.
+ *
+ * dart_layernorm: layer norm of s = x + residual (s = x where residual is
+ * NULL; the sum is rounded to the storage type first, and the norm is that of
+ * the rounded sum):
+ *   mu = mean(s) if center else 0,  inv = (mean((s - mu)^2) + eps)^-1/2,
+ *   out = (s - mu) inv (.) weight + bias
+ * (center = 0 without bias is the RMS norm).  Statistics are float.
+ *   x        [rows][x_row_stride], residual [rows][residual_row_stride] (or
+ *            NULL) storage dtype, channel i at element i of the row
+ *   weight, bias [dim] float, or NULL (ones, zeros)
+ *   out, sum [rows][dim] storage dtype; sum may be NULL, and is NULL where
+ *            residual is
+ * out or sum may be x or residual itself (the same pointer, row stride dim);
+ * any other overlap of an output is refused.  dim <= 16384, eps > 0.  Any
+ * alignment and stride of whole elements; rows that all lie on 16 bytes are
+ * faster.
+ */
+dart_status dart_layernorm(int64_t rows, int32_t dim, int32_t dtype, int32_t center, const void* x,
+                           int64_t x_row_stride, const void* residual, int64_t residual_row_stride,
+                           const float* weight, const float* bias, float eps, void* out, void* sum,
+                           void* stream);
+
+/*
+ * dart_layernorm_bwd: with xh = (x - mu) inv of the norm's input x (the
+ * forward's sum; its statistics are formed again) and g = dout (.) weight:
+ *   dx = inv (g - mean(g) [only if center] - xh mean(g xh)) + dsum
+ *   dweight = sum over rows of dout xh,   dbias = sum over rows of dout
+ * dsum is the gradient that reaches the sum past the norm (the residual
+ * stream's), so dx is the gradient of x and of residual alike.
+ *   x            as in dart_layernorm (dtype); dout, dsum (or NULL), dx
+ *                [rows][dim] grad_dtype: DART_FP32, or DART_BF16 with bf16 x
+ *   dweight, dbias [dim] float, or NULL
+ *   workspace    device buffer of >= dart_layernorm_bwd_workspace_bytes()
+ * dx may be dout or dsum itself; any other overlap is refused.  Sums in a
+ * fixed order.
+ */
+size_t dart_layernorm_bwd_workspace_bytes(int64_t rows, int32_t dim);
+dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t grad_dtype,
+                               int32_t center, const void* x, int64_t x_row_stride,
+                               const float* weight, float eps, const void* dout, const void* dsum,
+                               void* dx, float* dweight, float* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/*
+ * dart_token_logprobs: for each row l of `vocab` logits
+ *   row_max = max_j l_j,   log_sum = log sum_j exp(l_j - row_max),
+ *   logprob = (l_t - row_max) - log_sum   of the row's target t,
+ *   entropy = - sum_j p_j log p_j,        p_j = exp(l_j - row_max - log_sum),
+ *   top_ids, top_logprobs: the top_k largest logits, largest first, equal ones
+ *   by the lowest index (-0 equals 0; a NaN is above all).
+ * A row whose target is ignore_index has logprob 0; any other target outside
+ * [0, vocab) makes logprob NaN and reads nothing.  A logit of -infinity has
+ * probability 0.  A row of nothing else has row_max = log_sum = -infinity,
+ * entropy 0 and, for every token, logprob -infinity.  A logit of NaN or
+ * +infinity makes the row's log_sum, logprob and entropy NaN.
+ *   logits   [rows][row_stride] storage dtype, any alignment
+ *   targets  [rows] int64, or NULL (then logprob is NULL)
+ *   logprob, entropy, row_max, log_sum [rows] float, each may be NULL
+ *   top_ids [rows][top_k] int64, top_logprobs [rows][top_k] float; 0 <= top_k
+ *   <= min(vocab, DART_MAX_TOP_K), the pointers NULL where top_k = 0
+ *   workspace  device buffer of >= dart_token_logprobs_workspace_bytes() (may
+ *   be NULL where that is 0)
+ */
+#define DART_MAX_TOP_K 32
+size_t dart_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t dtype, int32_t top_k);
+dart_status dart_token_logprobs(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                const void* logits, const int64_t* targets, int64_t ignore_index,
+                                int32_t top_k, float* logprob, float* entropy, float* row_max,
+                                float* log_sum, int64_t* top_ids, float* top_logprobs,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * dart_token_logprobs_bwd: the gradient of
+ *   sum_r dlogprob_r logprob_r + dentropy_r entropy_r + dlse_r (row_max_r + log_sum_r)
+ * with respect to the logits (a row whose target is ignore_index has no
+ * logprob term):
+ *   dl_j = p_j (dlse - dlogprob - dentropy (log p_j + entropy)) + [j = t] dlogprob.
+ *   logits, targets, ignore_index as in the forward; row_max, log_sum and
+ *   (where dentropy is given) entropy the forward's results
+ *   dlogprob (needs targets), dentropy, dlse [rows] float, each may be NULL
+ *   dlogits [rows][dlogits_row_stride] grad_dtype: DART_FP32, or DART_BF16 with
+ *   bf16 logits; elements past vocab of a row are left as they are
+ * dlogits may be logits itself (the same pointer, type and stride); any other
+ * overlap is refused.
+ */
+dart_status dart_token_logprobs_bwd(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                    int32_t grad_dtype, const void* logits, const int64_t* targets,
+                                    int64_t ignore_index, const float* row_max,
+                                    const float* log_sum, const float* entropy,
+                                    const float* dlogprob, const float* dentropy,
+                                    const float* dlse, void* dlogits, int64_t dlogits_row_stride,
+                                    void* stream);
+
+/*
+ * dart_token_logprobs_grad: the forward and that gradient in one call, for a
+ * loss whose dlogprob, dentropy and dlse are known before (a mean over the
+ * tokens, say): the logits are read from memory once where a row fits a
+ * workgroup's registers.  Arguments as above; row_max, log_sum and, with dentropy, entropy must
+ * be given; dlogits may be logits itself.
+ */
+dart_status dart_token_logprobs_grad(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                     int32_t grad_dtype, const void* logits, const int64_t* targets,
+                                     int64_t ignore_index, int32_t top_k, const float* dlogprob,
+                                     const float* dentropy, const float* dlse, float* logprob,
+                                     float* entropy, float* row_max, float* log_sum,
+                                     int64_t* top_ids, float* top_logprobs, void* dlogits,
+                                     int64_t dlogits_row_stride, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/*
+ * dart_clip_grad_norm: the global norm of n tensors and their clipping,
+ *   norm = |scale| sqrt(sum over the tensors of sum g^2),
+ *   out_i = g_i scale c,   c = min(1, max_norm / (norm + 1e-6)).
+ * The squares are summed in 64 bits.  A NaN among the gradients makes norm and
+ * every out NaN; an infinity makes c = 0 (and itself NaN).  max_norm may be
+ * infinite (scaling alone).  dart_grad_norm computes norm alone.
+ *   grads, outs  HOST arrays of n device pointers; numels HOST array of n
+ *                element counts (0 allowed: the pointers are not used);
+ *                dtypes, out_dtypes HOST arrays of n dart_dtypes.  The arrays
+ *                may be freed when the call returns.
+ *   outs[i]      may be grads[i] itself, of the same type: in place (left
+ *                alone where scale c = 1); outputs that overlap anything else
+ *                are refused.  Any alignment of whole elements.
+ *   norm         device [1] float
+ *   workspace    device buffer of >= dart_grad_norm_workspace_bytes(n)
+ */
+size_t dart_grad_norm_workspace_bytes(int64_t n);
+dart_status dart_grad_norm(int64_t n, const void* const* grads, const int64_t* numels,
+                           const int32_t* dtypes, float scale, float* norm, void* workspace,
+                           size_t workspace_bytes, void* stream);
+dart_status dart_clip_grad_norm(int64_t n, const void* const* grads, void* const* outs,
+                                const int64_t* numels, const int32_t* dtypes,
+                                const int32_t* out_dtypes, float max_norm, float scale, float* norm,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
 /* Bytes of workspace dart_decode_step needs (dims->seqlen is ignored; the
  * worst case over positions that fit dims->mem_capacity is returned). */
 size_t dart_decode_workspace_bytes(const dart_dims* dims);

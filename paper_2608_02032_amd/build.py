@@ -22,6 +22,7 @@ LIB = os.path.join(HERE, "libdart.so")
 ARCH = "gfx950"
 
 SOURCES = ["scan.hip", "scan_f32.hip", "sma.hip", "sma_f32.hip", "sma_bwd.hip", "scan_bwd.hip", "scan_bwd_mfma.hip", "decode.hip", "block.hip",
+           "norm.hip", "logprobs.hip", "clip.hip",
            "dart_api.cpp", "profile.cpp"]
 
 COMMON_FLAGS = [

@@ -524,15 +524,16 @@ __global__ __launch_bounds__(LANES * COLS) void k_sum_parts(const float* __restr
     }
     if (i >= width) return;
     // items of K values: the first `keep` go to out ([item][keep]), the rest
-    // (at most one) to out2 ([item])
+    // to out2 ([item][K - keep])
     const int64_t item = i / K;
     const int k = (int)(i - item * K);
     if (k < keep) {
         if (out) out[item * keep + k] = s;
     } else if (out2) {
-        out2[item] = s;
+        out2[item * (K - keep) + k - keep] = s;
     }
 }
+}  // namespace
 void sum_parts(const float* part, int64_t nparts, int64_t width, float* out, int K, int keep, float* out2,
                hipStream_t st) {
     prof_begin("k_sum_parts", st);
@@ -543,6 +544,7 @@ void sum_parts(const float* part, int64_t nparts, int64_t width, float* out, int
             part, nparts, width, out, K, keep, out2);
     prof_end(st);
 }
+namespace {
 
 // dt = softplus(raw + bias): draw = ddt sigmoid(raw + bias), dbias = sum over
 // rows.  A block serves kDtRows rows of up to 256 heads: its threads tile

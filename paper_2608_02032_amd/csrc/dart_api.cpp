@@ -6,10 +6,13 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdint>
 #include <cstring>
+#include <new>
 
 #include "dart_internal.hpp"
 
@@ -88,6 +91,27 @@ dart::SmaArgs sma_args(const dart_sma_opts* o) {
 dart_status hip_status(hipError_t e, const char* what) {
     if (e != hipSuccess) return fail(DART_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
     return ok();
+}
+
+// The bytes that `rows` rows of `width` elements at a stride take, from p.
+struct Range {
+    uintptr_t a, b;  // first byte, one past the last
+    Range(const void* p, int64_t rows, int64_t stride, int64_t width, int dtype)
+        : a((uintptr_t)p), b(p && rows > 0 ? a + (uintptr_t)((rows - 1) * stride + width) * dart::elem_bytes(dtype) : a) {}
+    bool meets(const Range& o) const { return a < o.b && o.a < b; }
+};
+
+// rows x stride elements have to be addressable.
+bool too_large(int64_t rows, int64_t stride) { return rows > 0 && stride > ((int64_t)1 << 56) / rows; }
+
+dart_status check_dtypes(int dtype, int grad_dtype) {
+    if (dtype != DART_FP32 && dtype != DART_BF16)
+        return fail(DART_ERR_INVALID_ARG, "dtype must be DART_FP32 or DART_BF16 (got %d)", dtype);
+    if (grad_dtype != DART_FP32 && grad_dtype != DART_BF16)
+        return fail(DART_ERR_INVALID_ARG, "grad_dtype must be DART_FP32 or DART_BF16 (got %d)", grad_dtype);
+    if (grad_dtype == DART_BF16 && dtype == DART_FP32)
+        return fail(DART_ERR_UNSUPPORTED, "grad_dtype DART_BF16 needs dtype DART_BF16");
+    return DART_OK;
 }
 
 #define REQUIRE_PTR(p) \
@@ -393,6 +417,295 @@ dart_status dart_gated_rmsnorm_bwd(int64_t rows, int32_t dim, int32_t group, int
                                                      weight, eps, dout, dy, dz, dz_row_stride,
                                                      dweight, workspace, (hipStream_t)stream),
                       "dart_gated_rmsnorm_bwd launch");
+}
+
+// ---- the steps around the blocks ---------------------------------------------
+
+static dart_status check_norm(int64_t rows, int32_t dim, int32_t center, int64_t x_row_stride, float eps) {
+    if (rows < 0 || dim < 1) return fail(DART_ERR_INVALID_ARG, "rows must be >= 0 and dim >= 1");
+    if (dim > 16384) return fail(DART_ERR_UNSUPPORTED, "dim %d not supported (at most 16384)", dim);
+    if (center != 0 && center != 1) return fail(DART_ERR_INVALID_ARG, "center must be 0 or 1");
+    if (x_row_stride < dim)
+        return fail(DART_ERR_INVALID_ARG, "x_row_stride (%lld) < dim (%d)", (long long)x_row_stride, dim);
+    if (too_large(rows, x_row_stride)) return fail(DART_ERR_UNSUPPORTED, "too many rows");
+    if (!(eps > 0.0f)) return fail(DART_ERR_INVALID_ARG, "eps must be > 0");
+    return DART_OK;
+}
+
+dart_status dart_layernorm(int64_t rows, int32_t dim, int32_t dtype, int32_t center, const void* x,
+                           int64_t x_row_stride, const void* residual, int64_t residual_row_stride,
+                           const float* weight, const float* bias, float eps, void* out, void* sum,
+                           void* stream) {
+    dart_status st = check_norm(rows, dim, center, x_row_stride, eps);
+    if (st != DART_OK) return st;
+    st = check_dtypes(dtype, DART_FP32);
+    if (st != DART_OK) return st;
+    if (!residual && sum) return fail(DART_ERR_INVALID_ARG, "sum needs a residual");
+    if (residual && residual_row_stride < dim)
+        return fail(DART_ERR_INVALID_ARG, "residual_row_stride (%lld) < dim (%d)", (long long)residual_row_stride, dim);
+    if (residual && too_large(rows, residual_row_stride)) return fail(DART_ERR_UNSUPPORTED, "too many rows");
+    if (rows == 0) return ok();
+    REQUIRE_PTR(x);
+    REQUIRE_PTR(out);
+    const Range rx(x, rows, x_row_stride, dim, dtype), rr(residual, rows, residual_row_stride, dim, dtype);
+    const Range ro(out, rows, dim, dim, dtype), rs(sum, rows, dim, dim, dtype);
+    const Range rw(weight, 1, dim, dim, DART_FP32), rb(bias, 1, dim, dim, DART_FP32);
+    for (const Range* o : {&ro, &rs}) {
+        const bool is_x = o->a == rx.a && (x_row_stride == dim || rows == 1);
+        const bool is_r = o->a == rr.a && (residual_row_stride == dim || rows == 1);
+        if ((!is_x && o->meets(rx)) || (!is_r && o->meets(rr)) || o->meets(rw) || o->meets(rb))
+            return fail(DART_ERR_INVALID_ARG, "an output overlaps an input (only x or residual itself, at row stride dim, is allowed)");
+    }
+    if (ro.meets(rs)) return fail(DART_ERR_INVALID_ARG, "out overlaps sum");
+    return hip_status(dart::launch_layernorm(dtype, rows, dim, center, x, x_row_stride, residual,
+                                             residual_row_stride, weight, bias, eps, out, sum,
+                                             (hipStream_t)stream),
+                      "dart_layernorm launch");
+}
+
+size_t dart_layernorm_bwd_workspace_bytes(int64_t rows, int32_t dim) {
+    if (rows < 0 || dim < 1 || dim > 16384 || too_large(rows, dim)) return 0;
+    return dart::layernorm_bwd_workspace_bytes(rows, dim);
+}
+
+dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t grad_dtype,
+                               int32_t center, const void* x, int64_t x_row_stride,
+                               const float* weight, float eps, const void* dout, const void* dsum,
+                               void* dx, float* dweight, float* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    dart_status st = check_norm(rows, dim, center, x_row_stride, eps);
+    if (st != DART_OK) return st;
+    st = check_dtypes(dtype, grad_dtype);
+    if (st != DART_OK) return st;
+    if (rows > 0) {
+        REQUIRE_PTR(x);
+        REQUIRE_PTR(dout);
+        REQUIRE_PTR(dx);
+        REQUIRE_PTR(workspace);
+        const Range rx(x, rows, x_row_stride, dim, dtype), ro(dout, rows, dim, dim, grad_dtype);
+        const Range rs(dsum, rows, dim, dim, grad_dtype), rd(dx, rows, dim, dim, grad_dtype);
+        const Range rw(weight, 1, dim, dim, DART_FP32), rdw(dweight, 1, dim, dim, DART_FP32);
+        const Range rdb(dbias, 1, dim, dim, DART_FP32);
+        if (rd.meets(rx) || rd.meets(rw) || (rd.a != ro.a && rd.meets(ro)) || (rd.a != rs.a && rd.meets(rs)))
+            return fail(DART_ERR_INVALID_ARG, "dx overlaps an input (only dout or dsum itself is allowed)");
+        for (const Range* o : {&rdw, &rdb})
+            if (o->meets(rx) || o->meets(ro) || o->meets(rs) || o->meets(rd) || o->meets(rw))
+                return fail(DART_ERR_INVALID_ARG, "dweight or dbias overlaps another argument");
+        if (rdw.meets(rdb)) return fail(DART_ERR_INVALID_ARG, "dweight overlaps dbias");
+    }
+    const size_t need = dart::layernorm_bwd_workspace_bytes(rows, dim);
+    if (workspace_bytes < need)
+        return fail(DART_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
+    if (workspace && (uintptr_t)workspace % 16 != 0)
+        return fail(DART_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    return hip_status(dart::launch_layernorm_bwd(dtype, grad_dtype, rows, dim, center, x, x_row_stride,
+                                                 weight, eps, dout, dsum, dx, dweight, dbias,
+                                                 workspace, (hipStream_t)stream),
+                      "dart_layernorm_bwd launch");
+}
+
+static dart_status check_logits(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                int32_t grad_dtype, int32_t top_k) {
+    if (rows < 0 || vocab < 1) return fail(DART_ERR_INVALID_ARG, "rows must be >= 0 and vocab >= 1");
+    if (vocab > 2147483647LL) return fail(DART_ERR_UNSUPPORTED, "vocab must be < 2^31");
+    if (row_stride < vocab)
+        return fail(DART_ERR_INVALID_ARG, "row_stride (%lld) < vocab (%lld)", (long long)row_stride, (long long)vocab);
+    if (too_large(rows, row_stride)) return fail(DART_ERR_UNSUPPORTED, "too many rows");
+    if (top_k < 0 || top_k > vocab)
+        return fail(DART_ERR_INVALID_ARG, "top_k must be in [0, vocab] (got %d)", top_k);
+    if (top_k > DART_MAX_TOP_K)
+        return fail(DART_ERR_UNSUPPORTED, "top_k %d not supported (at most %d)", top_k, DART_MAX_TOP_K);
+    return check_dtypes(dtype, grad_dtype);
+}
+
+static dart_status check_dlogits(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                 int32_t grad_dtype, const void* logits, const void* dlogits,
+                                 int64_t dlogits_row_stride) {
+    if (dlogits_row_stride < vocab)
+        return fail(DART_ERR_INVALID_ARG, "dlogits_row_stride (%lld) < vocab (%lld)",
+                    (long long)dlogits_row_stride, (long long)vocab);
+    if (too_large(rows, dlogits_row_stride)) return fail(DART_ERR_UNSUPPORTED, "too many rows");
+    const Range rl(logits, rows, row_stride, vocab, dtype), rd(dlogits, rows, dlogits_row_stride, vocab, grad_dtype);
+    const bool same = logits == dlogits && dtype == grad_dtype && (row_stride == dlogits_row_stride || rows == 1);
+    if (!same && rl.meets(rd))
+        return fail(DART_ERR_INVALID_ARG, "dlogits overlaps logits (only logits itself, of the same type and stride, is allowed)");
+    return DART_OK;
+}
+
+size_t dart_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t dtype, int32_t top_k) {
+    if (check_logits(rows, vocab, vocab, dtype, DART_FP32, top_k) != DART_OK) return 0;
+    return dart::token_logprobs_workspace_bytes(rows, vocab, dtype, top_k);
+}
+
+// The forward's checks, then the launch with `grad` (or NULL).
+static dart_status run_token_logprobs(const dart::LogprobArgs& a, const dart::LogprobGrad* grad,
+                                      void* workspace, size_t workspace_bytes, void* stream,
+                                      const char* what) {
+    if (a.rows == 0) return ok();
+    if (!a.logits) return fail(DART_ERR_INVALID_ARG, "required pointer 'logits' is NULL");
+    if (a.logprob && !a.targets) return fail(DART_ERR_INVALID_ARG, "logprob needs targets");
+    if (a.top_k > 0 && (!a.top_ids || !a.top_logprobs))
+        return fail(DART_ERR_INVALID_ARG, "top_k > 0 needs top_ids and top_logprobs");
+    const size_t need = dart::token_logprobs_workspace_bytes(a.rows, a.vocab, a.dtype, a.top_k);
+    if (need > 0 && !workspace) return fail(DART_ERR_INVALID_ARG, "required pointer 'workspace' is NULL");
+    if (workspace_bytes < need)
+        return fail(DART_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
+    if (workspace && (uintptr_t)workspace % 16 != 0)
+        return fail(DART_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    return hip_status(dart::launch_token_logprobs(a, grad, workspace, (hipStream_t)stream), what);
+}
+
+dart_status dart_token_logprobs(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                const void* logits, const int64_t* targets, int64_t ignore_index,
+                                int32_t top_k, float* logprob, float* entropy, float* row_max,
+                                float* log_sum, int64_t* top_ids, float* top_logprobs,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+    dart_status st = check_logits(rows, vocab, row_stride, dtype, DART_FP32, top_k);
+    if (st != DART_OK) return st;
+    const dart::LogprobArgs a{rows, vocab, row_stride, dtype, top_k, logits, targets, ignore_index,
+                              logprob, entropy, row_max, log_sum, top_ids, top_logprobs};
+    return run_token_logprobs(a, nullptr, workspace, workspace_bytes, stream, "dart_token_logprobs launch");
+}
+
+dart_status dart_token_logprobs_bwd(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                    int32_t grad_dtype, const void* logits, const int64_t* targets,
+                                    int64_t ignore_index, const float* row_max,
+                                    const float* log_sum, const float* entropy,
+                                    const float* dlogprob, const float* dentropy,
+                                    const float* dlse, void* dlogits, int64_t dlogits_row_stride,
+                                    void* stream) {
+    dart_status st = check_logits(rows, vocab, row_stride, dtype, grad_dtype, 0);
+    if (st != DART_OK) return st;
+    st = check_dlogits(rows, vocab, row_stride, dtype, grad_dtype, logits, dlogits, dlogits_row_stride);
+    if (st != DART_OK) return st;
+    if (dlogprob && !targets) return fail(DART_ERR_INVALID_ARG, "dlogprob needs targets");
+    if (rows == 0) return ok();
+    REQUIRE_PTR(logits);
+    REQUIRE_PTR(row_max);
+    REQUIRE_PTR(log_sum);
+    REQUIRE_PTR(dlogits);
+    if (dentropy && !entropy) return fail(DART_ERR_INVALID_ARG, "dentropy needs entropy");
+    const dart::LogprobArgs a{rows, vocab, row_stride, dtype, 0, logits, targets, ignore_index,
+                              nullptr, const_cast<float*>(entropy), const_cast<float*>(row_max),
+                              const_cast<float*>(log_sum), nullptr, nullptr};
+    const dart::LogprobGrad g{grad_dtype, dlogits_row_stride, dlogprob, dentropy, dlse, dlogits};
+    return hip_status(dart::launch_token_logprobs_bwd(a, g, (hipStream_t)stream), "dart_token_logprobs_bwd launch");
+}
+
+dart_status dart_token_logprobs_grad(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
+                                     int32_t grad_dtype, const void* logits, const int64_t* targets,
+                                     int64_t ignore_index, int32_t top_k, const float* dlogprob,
+                                     const float* dentropy, const float* dlse, float* logprob,
+                                     float* entropy, float* row_max, float* log_sum,
+                                     int64_t* top_ids, float* top_logprobs, void* dlogits,
+                                     int64_t dlogits_row_stride, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+    dart_status st = check_logits(rows, vocab, row_stride, dtype, grad_dtype, top_k);
+    if (st != DART_OK) return st;
+    st = check_dlogits(rows, vocab, row_stride, dtype, grad_dtype, logits, dlogits, dlogits_row_stride);
+    if (st != DART_OK) return st;
+    if (dlogprob && !targets) return fail(DART_ERR_INVALID_ARG, "dlogprob needs targets");
+    if (rows > 0) {
+        REQUIRE_PTR(row_max);
+        REQUIRE_PTR(log_sum);
+        REQUIRE_PTR(dlogits);
+        if (dentropy && !entropy) return fail(DART_ERR_INVALID_ARG, "dentropy needs entropy");
+    }
+    const dart::LogprobArgs a{rows, vocab, row_stride, dtype, top_k, logits, targets, ignore_index,
+                              logprob, entropy, row_max, log_sum, top_ids, top_logprobs};
+    const dart::LogprobGrad g{grad_dtype, dlogits_row_stride, dlogprob, dentropy, dlse, dlogits};
+    return run_token_logprobs(a, &g, workspace, workspace_bytes, stream, "dart_token_logprobs_grad launch");
+}
+
+// Checks of a list of tensors; outs == NULL: they are only read.
+static dart_status check_grads(int64_t n, const void* const* grads, void* const* outs, const int64_t* numels,
+                               const int32_t* dtypes, const int32_t* out_dtypes, float scale,
+                               const float* norm, const void* workspace, size_t workspace_bytes) {
+    if (n < 0) return fail(DART_ERR_INVALID_ARG, "n must be >= 0 (got %lld)", (long long)n);
+    if (n > (1 << 24)) return fail(DART_ERR_UNSUPPORTED, "at most 2^24 tensors");
+    if (!std::isfinite(scale)) return fail(DART_ERR_INVALID_ARG, "scale must be finite");
+    REQUIRE_PTR(norm);
+    REQUIRE_PTR(workspace);
+    if (workspace_bytes < dart::grad_norm_workspace_bytes(n))
+        return fail(DART_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes,
+                    dart::grad_norm_workspace_bytes(n));
+    if ((uintptr_t)workspace % 16 != 0) return fail(DART_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    if (n == 0) return DART_OK;
+    REQUIRE_PTR(grads);
+    REQUIRE_PTR(numels);
+    REQUIRE_PTR(dtypes);
+    int64_t total = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (numels[i] < 0 || numels[i] > ((int64_t)1 << 42) || (total += numels[i]) > ((int64_t)1 << 42))
+            return fail(DART_ERR_INVALID_ARG, "tensor %lld: element counts must be >= 0, and at most 2^42 in all", (long long)i);
+        for (int d : {dtypes[i], outs ? out_dtypes[i] : dtypes[i]})
+            if (d != DART_FP32 && d != DART_BF16)
+                return fail(DART_ERR_INVALID_ARG, "tensor %lld: dtype must be DART_FP32 or DART_BF16 (got %d)", (long long)i, d);
+        if (numels[i] == 0) continue;
+        if (!grads[i] || (outs && !outs[i])) return fail(DART_ERR_INVALID_ARG, "tensor %lld: pointer is NULL", (long long)i);
+        if ((uintptr_t)grads[i] % dart::elem_bytes(dtypes[i]) != 0 ||
+            (outs && (uintptr_t)outs[i] % dart::elem_bytes(out_dtypes[i]) != 0))
+            return fail(DART_ERR_INVALID_ARG, "tensor %lld: not aligned to its elements", (long long)i);
+    }
+    if (!outs) return DART_OK;
+    // Whatever is written may meet nothing else: the ranges in order of their
+    // start, each against the furthest end so far.
+    struct Span {
+        uintptr_t a, b;
+        bool written;
+    };
+    Span* v = new (std::nothrow) Span[2 * (size_t)n];
+    if (!v) return fail(DART_ERR_INVALID_ARG, "out of host memory");
+    size_t m = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (numels[i] == 0) continue;
+        const Range g(grads[i], 1, 0, numels[i], dtypes[i]), o(outs[i], 1, 0, numels[i], out_dtypes[i]);
+        if (g.a != o.a || dtypes[i] != out_dtypes[i]) v[m++] = Span{g.a, g.b, false};
+        v[m++] = Span{o.a, o.b, true};
+    }
+    std::sort(v, v + m, [](const Span& p, const Span& q) { return p.a < q.a; });
+    uintptr_t end = 0, end_written = 0;
+    bool clash = false;
+    for (size_t i = 0; i < m; ++i) {
+        clash = clash || v[i].a < (v[i].written ? end : end_written);
+        end = std::max(end, v[i].b);
+        if (v[i].written) end_written = std::max(end_written, v[i].b);
+    }
+    delete[] v;
+    if (clash)
+        return fail(DART_ERR_INVALID_ARG, "an output overlaps another tensor (the same one twice?)");
+    return DART_OK;
+}
+
+size_t dart_grad_norm_workspace_bytes(int64_t n) {
+    if (n < 0 || n > (1 << 24)) return 0;
+    return dart::grad_norm_workspace_bytes(n);
+}
+
+dart_status dart_grad_norm(int64_t n, const void* const* grads, const int64_t* numels,
+                           const int32_t* dtypes, float scale, float* norm, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    const dart_status st = check_grads(n, grads, nullptr, numels, dtypes, nullptr, scale, norm, workspace, workspace_bytes);
+    if (st != DART_OK) return st;
+    return hip_status(dart::launch_clip_grad_norm(n, grads, nullptr, numels, dtypes, nullptr, INFINITY,
+                                                  scale, norm, workspace, (hipStream_t)stream),
+                      "dart_grad_norm launch");
+}
+
+dart_status dart_clip_grad_norm(int64_t n, const void* const* grads, void* const* outs,
+                                const int64_t* numels, const int32_t* dtypes,
+                                const int32_t* out_dtypes, float max_norm, float scale, float* norm,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+    if (!(max_norm >= 0.0f)) return fail(DART_ERR_INVALID_ARG, "max_norm must be >= 0");
+    if (n > 0) {
+        REQUIRE_PTR(outs);
+        REQUIRE_PTR(out_dtypes);
+    }
+    const dart_status st = check_grads(n, grads, outs, numels, dtypes, out_dtypes, scale, norm, workspace, workspace_bytes);
+    if (st != DART_OK) return st;
+    return hip_status(dart::launch_clip_grad_norm(n, grads, outs, numels, dtypes, out_dtypes, max_norm,
+                                                  scale, norm, workspace, (hipStream_t)stream),
+                      "dart_clip_grad_norm launch");
 }
 
 size_t dart_decode_workspace_bytes(const dart_dims* dims) {

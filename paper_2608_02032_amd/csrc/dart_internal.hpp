@@ -131,6 +131,54 @@ hipError_t launch_gated_rmsnorm_bwd(int dtype, int64_t rows, int D, int group, c
                                     const float* dout, float* dy, float* dz, int64_t dzstride,
                                     float* dw, void* ws, hipStream_t st);
 
+// out[item][k] = sum over p of part[p][item * K + k] (width = items * K) for
+// k < keep, out2[item][k - keep] for the others; either may be NULL.  In a fixed
+// order (block.hip).
+void sum_parts(const float* part, int64_t nparts, int64_t width, float* out, int K, int keep, float* out2,
+               hipStream_t st);
+
+// The norm of the residual stream (norm.hip); the backward's workspace holds
+// the partial sums of the weight's and the bias's gradient.
+hipError_t launch_layernorm(int dtype, int64_t rows, int D, int center, const void* x, int64_t xs,
+                            const void* res, int64_t rs, const float* w, const float* b, float eps,
+                            void* out, void* sum, hipStream_t st);
+size_t layernorm_bwd_workspace_bytes(int64_t rows, int D);
+hipError_t launch_layernorm_bwd(int dtype, int gdtype, int64_t rows, int D, int center, const void* x,
+                                int64_t xs, const float* w, float eps, const void* dout,
+                                const void* dsum, void* dx, float* dw, float* db, void* ws,
+                                hipStream_t st);
+
+// Log probabilities over a vocabulary (logprobs.hip).  `grad` adds the
+// gradient to the forward's call; the backward alone takes the forward's row
+// maximum, log of the sum and entropy.
+struct LogprobArgs {
+    int64_t rows, vocab, stride;
+    int dtype, top_k;
+    const void* logits;
+    const int64_t* targets;  // or NULL
+    int64_t ignore_index;
+    float *logprob, *entropy, *row_max, *log_sum;  // or NULL
+    int64_t* top_ids;
+    float* top_logprobs;
+};
+struct LogprobGrad {
+    int dtype;
+    int64_t stride;
+    const float *dlogprob, *dentropy, *dlse;  // or NULL
+    void* dlogits;
+};
+size_t token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int top_k);
+hipError_t launch_token_logprobs(const LogprobArgs& a, const LogprobGrad* grad, void* ws, hipStream_t st);
+hipError_t launch_token_logprobs_bwd(const LogprobArgs& a, const LogprobGrad& g, hipStream_t st);
+
+// Global gradient norm and clipping (clip.hip): the tensors' table and the
+// blocks' partial sums stand in the workspace.  out == NULL: the norm alone.
+size_t grad_norm_workspace_bytes(int64_t n);
+hipError_t launch_clip_grad_norm(int64_t n, const void* const* grads, void* const* outs,
+                                 const int64_t* numels, const int32_t* dtypes,
+                                 const int32_t* out_dtypes, float max_norm, float scale, float* norm,
+                                 void* ws, hipStream_t st);
+
 // Decode: per-split partial softmax statistics [B][H][nsplit][P+2] and the
 // SSM readout y_ssd [B][H][P] (float).
 constexpr int kDecodeMinMemPerSplit = 8;  // smallest split size the workspace allows

@@ -6,10 +6,12 @@ library has not been built, every call raises -- there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
 import threading
+from array import array
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +20,7 @@ LIB_PATH = os.path.join(HERE, "libdart.so")
 DART_OK, DART_ERR_INVALID_ARG, DART_ERR_UNSUPPORTED, DART_ERR_HIP = 0, 1, 2, 3
 DART_FP32, DART_BF16 = 0, 1
 DEFAULT_EPS = 1e-6
+MAX_TOP_K = 32
 
 
 class DartError(RuntimeError):
@@ -50,6 +53,10 @@ EXPORTS = ("dart_scan_workspace_bytes", "dart_ssd_chunk_scan", "dart_sma_workspa
            "dart_conv1d_silu_bwd_workspace_bytes", "dart_conv1d_silu_bwd",
            "dart_dt_softplus_bwd_workspace_bytes", "dart_dt_softplus_bwd",
            "dart_gated_rmsnorm_bwd_workspace_bytes", "dart_gated_rmsnorm_bwd",
+           "dart_layernorm", "dart_layernorm_bwd_workspace_bytes", "dart_layernorm_bwd",
+           "dart_token_logprobs_workspace_bytes", "dart_token_logprobs", "dart_token_logprobs_bwd",
+           "dart_token_logprobs_grad", "dart_grad_norm_workspace_bytes", "dart_grad_norm",
+           "dart_clip_grad_norm",
            "dart_decode_workspace_bytes", "dart_decode_step", "dart_decode_step_noalloc",
            "dart_decode_step_ragged", "dart_decode_handoff", "dart_decode_cache_elems", "dart_status_string", "dart_last_error",
            "dart_profile_enable", "dart_profile_filter", "dart_profile_flush", "dart_profile_count",
@@ -113,6 +120,28 @@ def load_library(path: str = LIB_PATH):
                                                P, P, i64, P, ctypes.c_float, P, P, P, i64, P, P, sz,
                                                P]
         lib.dart_gated_rmsnorm_bwd.restype = st
+        i32, f32 = ctypes.c_int32, ctypes.c_float
+        lib.dart_layernorm.argtypes = [i64, i32, i32, i32, P, i64, P, i64, P, P, f32, P, P, P]
+        lib.dart_layernorm.restype = st
+        lib.dart_layernorm_bwd_workspace_bytes.argtypes = [i64, i32]
+        lib.dart_layernorm_bwd_workspace_bytes.restype = sz
+        lib.dart_layernorm_bwd.argtypes = [i64, i32, i32, i32, i32, P, i64, P, f32, P, P, P, P, P, P, sz, P]
+        lib.dart_layernorm_bwd.restype = st
+        lib.dart_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32, i32]
+        lib.dart_token_logprobs_workspace_bytes.restype = sz
+        lib.dart_token_logprobs.argtypes = [i64, i64, i64, i32, P, P, i64, i32] + [P] * 7 + [sz, P]
+        lib.dart_token_logprobs.restype = st
+        lib.dart_token_logprobs_bwd.argtypes = [i64, i64, i64, i32, i32, P, P, i64] + [P] * 7 + [i64, P]
+        lib.dart_token_logprobs_bwd.restype = st
+        lib.dart_token_logprobs_grad.argtypes = [i64, i64, i64, i32, i32, P, P, i64, i32] + [P] * 10 + [
+            i64, P, sz, P]
+        lib.dart_token_logprobs_grad.restype = st
+        lib.dart_grad_norm_workspace_bytes.argtypes = [i64]
+        lib.dart_grad_norm_workspace_bytes.restype = sz
+        lib.dart_grad_norm.argtypes = [i64, P, P, P, f32, P, P, sz, P]
+        lib.dart_grad_norm.restype = st
+        lib.dart_clip_grad_norm.argtypes = [i64, P, P, P, P, P, f32, f32, P, P, sz, P]
+        lib.dart_clip_grad_norm.restype = st
         lib.dart_decode_workspace_bytes.argtypes = [D]
         lib.dart_decode_workspace_bytes.restype = sz
         lib.dart_decode_step.argtypes = [D, O, i64, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]
@@ -511,6 +540,321 @@ def gated_rmsnorm_bwd(y, z, dout, weight=None, group=None, eps=DEFAULT_EPS, dz=N
                                      _ptr(weight), float(eps), _ptr(dout), _ptr(dy), _ptr_rows(dz),
                                      dzs, _ptr(dw), _ptr(ws), ws.numel(), _stream(stream)))
     return {"dy": dy, "dz": dz, "dweight": dw}
+
+
+# --------------------------------------------------------------------------- #
+# around the blocks: the residual stream's norm, the vocabulary, the gradients
+# --------------------------------------------------------------------------- #
+
+def _one_device(*tensors):
+    """The tensors' device, which has to be one GPU, the current one: the
+    library launches on the current device's streams."""
+    torch = _torch()
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("tensor must live on the GPU")
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("tensors live on %s and %s" % (device, t.device))
+    if device is not None and device.index != torch.cuda.current_device():
+        raise ValueError("tensors live on %s, which is not the current device" % (device,))
+    return device
+
+
+def _allocating(stream):
+    """What is allocated for a call on another stream belongs to that stream's
+    memory, so that it is not handed on while the call still uses it."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
+def _row_stride(t, name) -> int:
+    """The common stride of the rows of t [..][D]."""
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError("%s rows must be contiguous" % name)
+    stride = None
+    for n, s in zip(t.shape[-2::-1], t.stride()[-2::-1]):
+        if n == 1:
+            continue
+        if stride is None:
+            stride, rows = s, n
+        elif s != stride * rows:
+            raise ValueError("%s rows must have a common stride" % name)
+        else:
+            rows *= n
+    return t.shape[-1] if stride is None else stride
+
+
+def _same(t, shape, dtype, name, contiguous=True):
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError("%s must be a %s tensor of shape %s" % (name, dtype, tuple(shape)))
+    if contiguous and not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def layernorm(x, weight=None, bias=None, residual=None, eps=DEFAULT_EPS, center=True, out=None,
+              sum_out=None, stream=None):
+    """Layer norm of x, or of s = x + residual, over the last axis
+    (dart_layernorm); center=False leaves the mean where it is (RMS norm).
+
+    x, residual [..][D] rows of a common stride (e.g. a slice of a wider
+    tensor), weight, bias [D] f32.  Returns out, or (out, s) with a residual; out
+    and sum_out may be x or residual (in place)."""
+    torch = _torch()
+    lib = load_library()
+    dtype = _dtype_num(x)
+    device = _one_device(x, weight, bias, residual, out, sum_out)
+    D = x.shape[-1]
+    rows = x.numel() // D if D else 0
+    f32 = torch.float32
+    _same(weight, (D,), f32, "weight")
+    _same(bias, (D,), f32, "bias")
+    _same(residual, x.shape, x.dtype, "residual", False)
+    _same(out, x.shape, x.dtype, "out")
+    _same(sum_out, x.shape, x.dtype, "sum_out")
+    if residual is None and sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    xs = _row_stride(x, "x")
+    rs = D if residual is None else _row_stride(residual, "residual")
+    with _allocating(stream):
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=device)
+        if residual is not None and sum_out is None:
+            sum_out = torch.empty(x.shape, dtype=x.dtype, device=device)
+    check(lib.dart_layernorm(rows, D, dtype, int(bool(center)), x.data_ptr(), xs, _addr(residual), rs,
+                             _addr(weight), _addr(bias), float(eps), out.data_ptr(), _addr(sum_out),
+                             _stream(stream)))
+    return out if residual is None else (out, sum_out)
+
+
+def layernorm_bwd(x, dout, weight=None, dsum=None, eps=DEFAULT_EPS, center=True, want_bias=False,
+                  dx=None, stream=None):
+    """Backward of layernorm (dart_layernorm_bwd) at the norm's input x (with a
+    residual the sum the forward returned), for the gradient dout of its output
+    and, optionally, dsum of the sum: both [..][D] float32, or bfloat16 with
+    bfloat16 x.  Returns {"dx" (of dout's type; also the residual's gradient),
+    "dweight" (None without weight), "dbias" (None unless want_bias)}; dx may be
+    dout or dsum."""
+    torch = _torch()
+    lib = load_library()
+    dtype = _dtype_num(x)
+    device = _one_device(x, dout, weight, dsum, dx)
+    D = x.shape[-1]
+    rows = x.numel() // D if D else 0
+    _same(weight, (D,), torch.float32, "weight")
+    gdtype = _dtype_num(dout)
+    _same(dout, x.shape, dout.dtype, "dout")
+    _same(dsum, x.shape, dout.dtype, "dsum")
+    _same(dx, x.shape, dout.dtype, "dx")
+    xs = _row_stride(x, "x")
+    with _allocating(stream):
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=dout.dtype, device=device)
+        dw = torch.empty((D,), dtype=torch.float32, device=device) if weight is not None else None
+        db = torch.empty((D,), dtype=torch.float32, device=device) if want_bias else None
+        ws = _workspace(lib.dart_layernorm_bwd_workspace_bytes(rows, D), device)
+    check(lib.dart_layernorm_bwd(rows, D, dtype, gdtype, int(bool(center)), x.data_ptr(), xs,
+                                 _addr(weight), float(eps), dout.data_ptr(), _addr(dsum),
+                                 dx.data_ptr(), _addr(dw), _addr(db), ws.data_ptr(), ws.numel(),
+                                 _stream(stream)))
+    return {"dx": dx, "dweight": dw, "dbias": db}
+
+
+def _logits_args(logits, targets, *others):
+    torch = _torch()
+    device = _one_device(logits, targets, *others)
+    V = logits.shape[-1]
+    lead = tuple(logits.shape[:-1])
+    _same(targets, lead, torch.int64, "targets")
+    return device, lead, logits.numel() // V if V else 0, V, _row_stride(logits, "logits")
+
+
+def _dlogits(dlogits, logits, grad_dtype, stride):
+    """The gradient's tensor: rows at the stride of the logits', so that their
+    alignment is the logits' too."""
+    torch = _torch()
+    if dlogits is not None:
+        if dlogits.shape != logits.shape:
+            raise ValueError("dlogits must have the shape of logits")
+        return dlogits, _row_stride(dlogits, "dlogits")
+    dtype = logits.dtype if grad_dtype is None else grad_dtype
+    V = logits.shape[-1]
+    buf = torch.empty(tuple(logits.shape[:-1]) + (stride,), dtype=dtype, device=logits.device)
+    return (buf if stride == V else buf[..., :V]), stride
+
+
+def _token_logprobs(logits, targets, top_k, ignore_index, stream, grad=None):
+    torch = _torch()
+    lib = load_library()
+    others = () if grad is None else tuple(grad[k] for k in ("dlogprob", "dentropy", "dlse", "dlogits"))
+    device, lead, rows, V, stride = _logits_args(logits, targets, *others)
+    dtype = _dtype_num(logits)
+    top_k = int(top_k)
+    f32 = dict(dtype=torch.float32, device=device)
+    if grad is not None:
+        for k in ("dlogprob", "dentropy", "dlse"):
+            _same(grad[k], lead, torch.float32, k)
+    with _allocating(stream):
+        r = {"logprob": torch.empty(lead, **f32) if targets is not None else None,
+             "entropy": torch.empty(lead, **f32), "row_max": torch.empty(lead, **f32),
+             "log_sum": torch.empty(lead, **f32), "top_ids": None, "top_logprobs": None}
+        if top_k > 0:
+            r["top_ids"] = torch.empty(lead + (top_k,), dtype=torch.int64, device=device)
+            r["top_logprobs"] = torch.empty(lead + (top_k,), **f32)
+        ws = _workspace(lib.dart_token_logprobs_workspace_bytes(rows, V, dtype, top_k), device)
+        if grad is not None:
+            r["dlogits"], ds = _dlogits(grad["dlogits"], logits, grad["dtype"], stride)
+    fwd = [_addr(r[k]) for k in ("logprob", "entropy", "row_max", "log_sum", "top_ids", "top_logprobs")]
+    if grad is None:
+        check(lib.dart_token_logprobs(rows, V, stride, dtype, logits.data_ptr(), _addr(targets),
+                                      int(ignore_index), top_k, *fwd, ws.data_ptr(), ws.numel(),
+                                      _stream(stream)))
+    else:
+        check(lib.dart_token_logprobs_grad(
+            rows, V, stride, dtype, _dtype_num(r["dlogits"]), logits.data_ptr(), _addr(targets),
+            int(ignore_index), top_k, _addr(grad["dlogprob"]), _addr(grad["dentropy"]),
+            _addr(grad["dlse"]), *fwd, r["dlogits"].data_ptr(), ds, ws.data_ptr(), ws.numel(),
+            _stream(stream)))
+    return r
+
+
+def token_logprobs(logits, targets=None, top_k=0, ignore_index=-100, stream=None):
+    """Log probabilities over the last axis of logits [..][V]
+    (dart_token_logprobs): a dict of float32 tensors [..] logprob (of targets
+    [..] int64; 0 where the target is ignore_index; None without targets),
+    entropy, row_max and log_sum (row_max + log_sum is the log of the sum of the
+    exponentials), and of the top_k most probable tokens, ties by the lowest
+    index, top_ids [..][top_k] int64 and top_logprobs (None where top_k is 0).
+
+    The rows of logits have a common stride (e.g. the first V columns of a padded
+    vocabulary)."""
+    return _token_logprobs(logits, targets, top_k, ignore_index, stream)
+
+
+def token_logprobs_bwd(logits, row_max, log_sum, targets=None, dlogprob=None, entropy=None,
+                       dentropy=None, dlse=None, ignore_index=-100, dlogits=None, grad_dtype=None,
+                       stream=None):
+    """Backward of token_logprobs (dart_token_logprobs_bwd) from its results
+    row_max, log_sum and, where dentropy is given, entropy: the gradient of
+    sum(dlogprob * logprob + dentropy * entropy + dlse * (row_max + log_sum)).
+    Returns dlogits, of grad_dtype (default: the logits' type; float32 or, with
+    bfloat16 logits, bfloat16); dlogits may be logits (in place)."""
+    torch = _torch()
+    lib = load_library()
+    device, lead, rows, V, stride = _logits_args(logits, targets, row_max, log_sum, entropy, dlogprob,
+                                                 dentropy, dlse, dlogits)
+    for t, nm in ((row_max, "row_max"), (log_sum, "log_sum"), (entropy, "entropy"),
+                  (dlogprob, "dlogprob"), (dentropy, "dentropy"), (dlse, "dlse")):
+        _same(t, lead, torch.float32, nm)
+    with _allocating(stream):
+        dlogits, ds = _dlogits(dlogits, logits, grad_dtype, stride)
+    check(lib.dart_token_logprobs_bwd(rows, V, stride, _dtype_num(logits), _dtype_num(dlogits),
+                                      logits.data_ptr(), _addr(targets), int(ignore_index),
+                                      row_max.data_ptr(), log_sum.data_ptr(), _addr(entropy),
+                                      _addr(dlogprob), _addr(dentropy), _addr(dlse),
+                                      dlogits.data_ptr(), ds, _stream(stream)))
+    return dlogits
+
+
+def token_logprobs_grad(logits, targets, dlogprob, dentropy=None, dlse=None, top_k=0,
+                        ignore_index=-100, dlogits=None, grad_dtype=None, stream=None):
+    """token_logprobs and token_logprobs_bwd in one call, for a loss whose
+    gradients dlogprob, dentropy, dlse [..] float32 are known before
+    (dart_token_logprobs_grad): token_logprobs' dict with "dlogits" added."""
+    return _token_logprobs(logits, targets, top_k, ignore_index, stream,
+                           {"dlogprob": dlogprob, "dentropy": dentropy, "dlse": dlse,
+                            "dlogits": dlogits, "dtype": grad_dtype})
+
+
+def _dense(t) -> bool:
+    """Whether t's elements fill one range of memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    n = 1
+    for s, d in sorted((s, d) for s, d in zip(t.stride(), t.shape) if d != 1):
+        if s != n:
+            return False
+        n *= d
+    return True
+
+
+def _tensor_list(tensors, name):
+    """(pointers, element counts, types) of a list of dense tensors."""
+    torch = _torch()
+    types = {torch.float32: DART_FP32, torch.bfloat16: DART_BF16}
+    ptrs, numels, dtypes = array("q"), array("q"), array("i")
+    device = tensors[0].device if tensors else None
+    for t in tensors:
+        if t.device != device:
+            raise ValueError("%s live on %s and %s" % (name, device, t.device))
+        code = types.get(t.dtype)
+        if code is None:
+            raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+        if not t.is_contiguous() and not _dense(t):
+            raise ValueError("%s must be dense (no gaps, no repeated elements)" % name)
+        ptrs.append(t.data_ptr())
+        numels.append(t.numel())
+        dtypes.append(code)
+    return ptrs, numels, dtypes
+
+
+def _host(a):
+    return a.buffer_info()[0] if a is not None and len(a) else None
+
+
+def grad_norm(grads, scale=1.0, stream=None):
+    """|scale| times the 2-norm over all elements of the tensors (dart_grad_norm):
+    a float32 tensor of no dimensions."""
+    return _clip(list(grads), None, None, scale, stream)
+
+
+def clip_grad_norm(grads, max_norm, scale=1.0, out=None, stream=None):
+    """Scale the gradients by `scale` and by min(1, max_norm / (norm + 1e-6)),
+    norm being that of the scaled ones (dart_clip_grad_norm); in place, or into
+    the tensors `out` of the same shapes, float32 or bfloat16 each.  Returns norm,
+    a float32 tensor of no dimensions: nothing waits for the GPU.  Gradients and
+    outputs are dense; no two outputs overlap."""
+    grads = list(grads)
+    return _clip(grads, grads if out is None else list(out), float(max_norm), scale, stream)
+
+
+def _clip(grads, out, max_norm, scale, stream):
+    torch = _torch()
+    lib = load_library()
+    n = len(grads)
+    ptrs, numels, dtypes = _tensor_list(grads, "gradients")
+    device = _one_device(*grads[:1]) or torch.device("cuda", torch.cuda.current_device())
+    optrs, odtypes = ptrs, dtypes
+    if out is not None and out is not grads:
+        if len(out) != n:
+            raise ValueError("%d outputs for %d gradients" % (len(out), n))
+        optrs, onumels, odtypes = _tensor_list(out, "outputs")
+        _one_device(*grads[:1], *out[:1])
+        for g, o in zip(grads, out):
+            if g.shape != o.shape or (g.stride() != o.stride() and not (g.is_contiguous() and o.is_contiguous())):
+                raise ValueError("an output must have its gradient's shape and order of elements")
+    with _allocating(stream):
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        ws = _workspace(lib.dart_grad_norm_workspace_bytes(n), device)
+    if out is None:
+        check(lib.dart_grad_norm(n, _host(ptrs), _host(numels), _host(dtypes), float(scale),
+                                 norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    else:
+        check(lib.dart_clip_grad_norm(n, _host(ptrs), _host(optrs), _host(numels), _host(dtypes),
+                                      _host(odtypes), max_norm, float(scale), norm.data_ptr(),
+                                      ws.data_ptr(), ws.numel(), _stream(stream)))
+    return norm
 
 
 def decode_step(pos, x, dt, A, Bm, Cm, q, e, z, h_state, chunk_acc, mem_cache, chunk,

@@ -1,0 +1,389 @@
+"""Log probabilities, entropy, best alternatives and their gradient against
+the definitions in 64 bits.
+
+Bounds, u = 2^-24 half a step of float.  A term exp(d), d = l - max, is off by
+the rounding of d, of d log2(e) and of the exponential: (2 |d| + 4) u of
+itself, weighted by itself; a sum of V terms rounds at most 64 times along a
+path beside trees: log_sum is off by at most K u, K = 64 + 4 + 2 (mean |d|
+under p <= 40) < 256 in all, beside its own half step; c / s (the entropy's
+other half, a mean of d) likewise relative to itself.  A log probability adds
+half steps of d and of the result.  p = exp(q), q = (l - max) - log_sum, is off
+by K u + (2 |q| + 4) u of itself.  A bf16 gradient adds half a step, 2^-8."""
+import numpy as np
+import pytest
+
+from paper_2608_02032_amd import dart
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+STEP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8}
+K = 256
+IGNORE = -100
+
+
+def tensor(a, dtype="fp32"):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+
+
+def ids(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int64).reshape(np.shape(a))).cuda()
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def reference(l, t, k):
+    """l [R][V] 64-bit, t [R] or None: the definitions, -inf and empty rows as documented."""
+    R, V = l.shape
+    with np.errstate(all="ignore"):
+        m = l.max(1)
+        none = np.isneginf(m)
+        d = l - np.where(none, 0.0, m)[:, None]
+        e = np.exp(d)
+        s = e.sum(1)
+        ls = np.where(none, -np.inf, np.log(s))
+        z = np.where(none, 0.0, ls)
+        q = d - z[:, None]
+        p = e / np.where(none, 1.0, s)[:, None]
+        H = -np.where(p > 0, p * np.where(p > 0, q, 0.0), 0.0).sum(1)
+        mean_d = np.where(p > 0, p * np.where(p > 0, np.abs(d), 0.0), 0.0).sum(1)
+    out = {"row_max": m, "log_sum": ls, "entropy": H, "q": q, "p": p, "d": d, "mean_d": mean_d}
+    if t is not None:
+        out["logprob"] = np.array([0.0 if t[r] == IGNORE else q[r, t[r]] for r in range(R)])
+    if k:
+        order = np.argsort(-l, axis=1, kind="stable")[:, :k]
+        out["top_ids"] = order
+        out["top_logprobs"] = np.take_along_axis(q, order, 1)
+    return out
+
+
+def close(got, ref, bound, what):
+    got = f64(got)
+    assert got.shape == ref.shape, what
+    fin = np.isfinite(ref)
+    assert np.array_equal(got[~fin], ref[~fin]), what + ": infinities"
+    d = np.abs(got[fin] - ref[fin])
+    b = np.broadcast_to(bound, ref.shape)[fin]
+    bad = ~(d <= b)
+    print("  %-12s worst |d|/bound %.3f" % (what, float((d / np.maximum(b, 1e-300)).max()) if d.size else 0.0), flush=True)
+    assert not bad.any(), "%s: %d of %d outside" % (what, bad.sum(), bad.size)
+
+
+def check_forward(logits, t, r, k, lead=None):
+    V = logits.shape[-1]
+    ref = reference(f64(logits).reshape(-1, V), None if t is None else t.reshape(-1), k)
+    shape = logits.shape[:-1]
+    fin = lambda a: np.where(np.isfinite(a), np.abs(a), 0.0)  # noqa: E731
+    als = K * U + U * fin(ref["log_sum"])
+    assert np.array_equal(f64(r["row_max"]).reshape(-1), ref["row_max"]), "row_max"
+    close(r["log_sum"].reshape(-1), ref["log_sum"], als, "log_sum")
+    close(r["entropy"].reshape(-1), ref["entropy"], als + K * U * ref["mean_d"] + U * ref["entropy"], "entropy")
+    if t is not None:
+        close(r["logprob"].reshape(-1), ref["logprob"], als + 4 * U * (fin(ref["logprob"]) + fin(ref["log_sum"])), "logprob")
+    if k:
+        assert tuple(r["top_ids"].shape) == tuple(shape) + (k,)
+        assert np.array_equal(r["top_ids"].cpu().numpy().reshape(-1, k), ref["top_ids"]), "top_ids"
+        b = als[:, None] + 4 * U * (fin(ref["top_logprobs"]) + fin(ref["log_sum"])[:, None])
+        close(r["top_logprobs"].reshape(-1, k), ref["top_logprobs"], b, "top_logprobs")
+    else:
+        assert r["top_ids"] is None and r["top_logprobs"] is None
+    return ref
+
+
+def check_grad(ref, t, dlp, dent, dlse, got, gdtype):
+    R, V = ref["p"].shape
+    col = lambda a: np.zeros((R, 1)) if a is None else f64(a).reshape(R, 1)  # noqa: E731
+    has = np.zeros(R, bool) if t is None else t.reshape(-1) != IGNORE
+    a, h, z = col(dlp) * has[:, None], col(dent), col(dlse)
+    p, q, H = ref["p"], ref["q"], ref["entropy"][:, None]
+    qs = np.where(p > 0, np.where(np.isfinite(q), q, 0.0), 0.0)
+    ref_g = p * (z - a - h * (qs + H))
+    for r in np.flatnonzero(has):
+        ref_g[r, t.reshape(-1)[r]] += a[r, 0]
+    scale = np.abs(a) + np.abs(z) + np.abs(h) * (np.abs(qs) + H + ref["mean_d"][:, None])
+    rel = 2 * K * U + 8 * U * np.abs(qs)
+    bound = STEP[gdtype] * np.abs(ref_g) + p * scale * rel + U * np.abs(a) * (np.abs(ref_g) > 0) * 4 + 1e-37
+    close(got.reshape(R, V), ref_g, bound, "dlogits")
+
+
+def rand_logits(rng, R, V, dtype, scale=2.5):
+    return rng.standard_normal((R, V)) * scale
+
+
+VOCABS = [1, 2, 3, 7, 8, 9, 64, 127, 128, 129, 500, 1000, 2047, 2048, 2049, 4096, 5003, 10000, 16384, 32001, 50257, 65537, 131072, 200001]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", VOCABS)
+def test_vocabularies(dtype, V):
+    rng = np.random.default_rng(V)
+    for R, k in ((1, min(V, 20)), (5, min(V, 1)), (3, 0), (67 if V <= 5003 else 2, min(V, 32))):
+        print("\n[gpu-case] logprobs %s R=%d V=%d k=%d" % (dtype, R, V, k), flush=True)
+        l = tensor(rand_logits(rng, R, V, dtype), dtype)
+        t = rng.integers(0, V, R)
+        t[::3] = IGNORE
+        r = dart.token_logprobs(l, ids(t), top_k=k)
+        ref = check_forward(l, t, r, k)
+        dlp, dent, dlse = (tensor(rng.standard_normal(R)) for _ in range(3))
+        for gdtype in {"fp32", dtype}:
+            import torch
+            gt = torch.bfloat16 if gdtype == "bf16" else torch.float32
+            for use in ((dlp, None, None), (dlp, dent, dlse), (None, dent, None)):
+                g = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], targets=ids(t), dlogprob=use[0], entropy=r["entropy"],
+                                            dentropy=use[1], dlse=use[2], grad_dtype=gt)
+                check_grad(ref, t, use[0], use[1], use[2], g, gdtype)
+                one = dart.token_logprobs_grad(l, ids(t), use[0], dentropy=use[1], dlse=use[2], top_k=k, grad_dtype=gt)
+                check_forward(l, t, one, k)
+                check_grad(ref, t, use[0], use[1], use[2], one["dlogits"], gdtype)
+
+
+@pytest.mark.parametrize("R,V", [(300, 40), (257, 128), (4097, 130), (520, 3001), (600, 20011), (300, 50257), (64, 60000), (33, 100003)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_rows(dtype, R, V):
+    import torch
+    rng = np.random.default_rng(R + V)
+    print("\n[gpu-case] logprobs many rows %s R=%d V=%d" % (dtype, R, V), flush=True)
+    l = tensor(rng.standard_normal((R, V)).astype(np.float32) * 3, dtype)
+    t = rng.integers(0, V, R)
+    t[rng.random(R) < 0.3] = IGNORE
+    r = dart.token_logprobs(l, ids(t), top_k=5)
+    # every row's statistics and alternatives, a few rows' gradient
+    ref = check_forward(l, t, r, 5)
+    dlp = tensor(rng.standard_normal(R))
+    g = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], targets=ids(t), dlogprob=dlp)
+    one = dart.token_logprobs_grad(l, ids(t), dlp, top_k=5)
+    pick = np.unique(np.concatenate([np.arange(3), rng.integers(0, R, 20), [R - 1]]))
+    sub = {k: v[pick] for k, v in ref.items()}
+    where = torch.from_numpy(pick).cuda()
+    check_grad(sub, t[pick], dlp[where], None, None, g[where], dtype)
+    check_grad(sub, t[pick], dlp[where], None, None, one["dlogits"][where], dtype)
+    for k in ("logprob", "entropy", "row_max", "log_sum", "top_ids"):
+        assert one[k].equal(r[k]) or np.abs(f64(one[k]) - f64(r[k])).max() <= 2 * K * U * 20, k
+
+
+def test_leading_axes_no_rows_and_no_targets():
+    import torch
+    rng = np.random.default_rng(2)
+    l = tensor(rng.standard_normal((3, 4, 50)))
+    t = rng.integers(0, 50, (3, 4))
+    r = dart.token_logprobs(l, ids(t), top_k=2)
+    assert r["logprob"].shape == (3, 4) and r["top_ids"].shape == (3, 4, 2)
+    check_forward(l, t, r, 2)
+    r = dart.token_logprobs(l, top_k=2)
+    assert r["logprob"] is None
+    check_forward(l, None, r, 2)
+    g = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], dlse=torch.ones(3, 4, device="cuda"))
+    check_grad(reference(f64(l).reshape(-1, 50), None, 0), None, None, None, torch.ones(12, device="cuda"), g, "fp32")
+    r = dart.token_logprobs(l[0, 0], ids(np.array(3)))
+    assert r["logprob"].shape == ()
+    e = torch.empty(0, 50, device="cuda")
+    z = torch.empty(0, dtype=torch.int64, device="cuda")
+    r = dart.token_logprobs_grad(e, z, torch.empty(0, device="cuda"), top_k=3)
+    assert r["dlogits"].shape == (0, 50) and r["top_ids"].shape == (0, 3)
+
+
+def hard_rows(V):
+    """Rows where statistics and order can go wrong."""
+    rng = np.random.default_rng(V)
+    low = -3.3895313892515355e+38   # bfloat16's lowest value
+    rows = [np.full(V, -np.inf), np.zeros(V), np.full(V, low), np.full(V, 1e4), np.full(V, -1e30)]
+    a = rng.standard_normal(V)
+    a[: V // 2] = -np.inf
+    rows.append(a)
+    a = np.full(V, -np.inf)
+    a[V - 1] = 3.0                        # one token left
+    rows.append(a)
+    a = rng.standard_normal(V)
+    a[V // 3:] = low                      # masked with the lowest value instead
+    rows.append(a)
+    a = np.full(V, -5.0)
+    a[V // 2] = 80.0                      # certain
+    rows.append(a)
+    rows.append(np.linspace(-30, 30, V))  # rising, falling: every vector a new maximum, or none
+    rows.append(np.linspace(30, -30, V))
+    rows.append(np.round(rng.standard_normal(V)))           # many ties
+    rows.append(np.where(np.arange(V) % 2, -0.0, 0.0))      # -0 ties with 0
+    a = np.full(V, -20.0)
+    a[::256] = 10.0 + np.arange(len(a[::256])) % 7           # all of the best where one thread of a workgroup looks
+    rows.append(a)
+    a = np.full(V, -20.0)
+    a[::2048] = 5.0 - np.arange(len(a[::2048]))
+    a[1::2048] = 5.5 - np.arange(len(a[1::2048]))
+    rows.append(a)
+    rows.append(1e4 + rng.standard_normal(V) * 50)          # a large common part
+    a = np.full(V, low)
+    a[: min(V, 4)] = -np.inf
+    rows.append(a)
+    return np.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V,R", [(5, 1), (33, 1), (600, 1), (5000, 1), (50257, 1), (131073, 1), (5000, 40), (50257, 12)])
+def test_hard_rows(dtype, V, R):
+    print("\n[gpu-case] logprobs hard rows %s V=%d x%d" % (dtype, V, R), flush=True)
+    a = np.tile(hard_rows(V), (R, 1))
+    l = tensor(a, dtype)
+    t = np.arange(len(a)) * 7 % V
+    for k in {min(V, 1), min(V, 20), min(V, 32)}:
+        r = dart.token_logprobs(l, ids(t), top_k=k)
+        ref = check_forward(l, t, r, k)
+    dlp, dent = tensor(np.ones(len(a))), tensor(np.full(len(a), 0.5))
+    g = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], targets=ids(t), dlogprob=dlp, entropy=r["entropy"], dentropy=dent)
+    check_grad(ref, t, dlp, dent, None, g, dtype)
+    one = dart.token_logprobs_grad(l, ids(t), dlp, dentropy=dent, top_k=k)
+    check_forward(l, t, one, k)
+    check_grad(ref, t, dlp, dent, None, one["dlogits"], dtype)
+
+
+@pytest.mark.parametrize("V", [100, 5000, 60001])
+@pytest.mark.parametrize("R", [4, 700])
+def test_nonfinite_and_bad_targets(V, R):
+    """NaN and +infinity spoil their own row alone; a target out of range gives NaN and reads nothing."""
+    import torch
+    rng = np.random.default_rng(V)
+    a = rng.standard_normal((R, V))
+    good = tensor(a, "bf16")
+    l = good.clone()
+    l[1, V // 2], l[2, V - 1] = float("nan"), float("inf")
+    t = rng.integers(0, V, R)
+    bad = t.copy()
+    bad[3] = V
+    bad[0] = -7
+    x, y = dart.token_logprobs(good, ids(t), top_k=4), dart.token_logprobs(l, ids(bad), top_k=4)
+    rest = torch.arange(4, R, device="cuda")
+    for k in ("logprob", "entropy", "log_sum", "row_max", "top_ids", "top_logprobs"):
+        assert x[k][rest].equal(y[k][rest]), k
+    for k in ("logprob", "entropy", "log_sum"):
+        assert bool(torch.isnan(y[k][1:3]).all()), k
+    assert bool(torch.isnan(y["logprob"][[0, 3]]).all()) and bool(torch.isfinite(y["entropy"][[0, 3]]).all())
+    assert int(y["top_ids"][1, 0]) == V // 2 and int(y["top_ids"][2, 0]) == V - 1
+    assert bool(((y["top_ids"] >= 0) & (y["top_ids"] < V)).all())
+    dlp = tensor(rng.standard_normal(R))
+    g = dart.token_logprobs_bwd(good, x["row_max"], x["log_sum"], targets=ids(t), dlogprob=dlp)
+    h = dart.token_logprobs_bwd(l, y["row_max"], y["log_sum"], targets=ids(bad), dlogprob=dlp)
+    one = dart.token_logprobs_grad(l, ids(bad), dlp)["dlogits"]
+    for o in (h, one):
+        assert bool(torch.isnan(o[:4]).any(1).all()) and bool(torch.isfinite(o[4:].float()).all())
+    assert g[4:].equal(h[4:])
+    # an ignored row has no gradient, whatever it holds
+    skip = bad.copy()
+    skip[:4] = IGNORE
+    for o in (dart.token_logprobs_bwd(l, y["row_max"], y["log_sum"], targets=ids(skip), dlogprob=dlp),
+              dart.token_logprobs_grad(l, ids(skip), dlp)["dlogits"]):
+        assert not bool(o[:4].float().any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V,pad,first,R", [(50, 14, 0, 9), (1001, 5, 0, 9), (1001, 4, 3, 9), (50257, 47, 1, 3), (50257, 0, 5, 3),
+                                           (3000, 8, 8, 700), (3001, 2, 1, 700)])
+def test_strides_alignment_and_in_place(dtype, V, pad, first, R):
+    import torch
+    print("\n[gpu-case] logprobs stride %s V=%d pad=%d first=%d R=%d" % (dtype, V, pad, first, R), flush=True)
+    rng = np.random.default_rng(V + pad)
+    wide = tensor(rng.standard_normal((R, V + pad + first)) * 2, dtype)
+    if pad:
+        wide[:, first + V:] = 1e9      # what lies past the vocabulary is not read
+    l = wide[:, first:first + V]
+    t = rng.integers(0, V, R)
+    r = dart.token_logprobs(l, ids(t), top_k=7)
+    ref = check_forward(l, t, r, 7)
+    dlp, dent = tensor(rng.standard_normal(R)), tensor(rng.standard_normal(R))
+    a = dict(targets=ids(t), dlogprob=dlp, entropy=r["entropy"], dentropy=dent)
+    own = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], **a)
+    check_grad(ref, t, dlp, dent, None, own, dtype)
+    # a gradient of another stride and alignment
+    buf = torch.full((R, V + 9), 7.0, dtype=l.dtype, device="cuda")
+    g = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], dlogits=buf[:, 2:2 + V], **a)
+    assert g.equal(own) and bool((buf[:, :2] == 7.0).all()) and bool((buf[:, 2 + V:] == 7.0).all())
+    buf.fill_(7.0)
+    one = dart.token_logprobs_grad(l, ids(t), dlp, dentropy=dent, top_k=7, dlogits=buf[:, 2:2 + V])
+    check_grad(ref, t, dlp, dent, None, one["dlogits"], dtype)
+    assert bool((buf[:, :2] == 7.0).all()) and bool((buf[:, 2 + V:] == 7.0).all())
+    # in place
+    for fused in (False, True):
+        copy = wide.clone()
+        c = copy[:, first:first + V]
+        if fused:
+            assert dart.token_logprobs_grad(c, ids(t), dlp, dentropy=dent, top_k=7, dlogits=c)["top_ids"].equal(r["top_ids"])
+        else:
+            dart.token_logprobs_bwd(c, r["row_max"], r["log_sum"], dlogits=c, **a)
+        check_grad(ref, t, dlp, dent, None, c, dtype)
+        assert copy[:, :first].equal(wide[:, :first]) and copy[:, first + V:].equal(wide[:, first + V:])
+
+
+def test_gradient_against_differences():
+    rng = np.random.default_rng(4)
+    R, V = 3, 17
+    l = (rng.standard_normal((R, V)) * 2).astype(np.float32).astype(np.float64)
+    t = np.array([2, IGNORE, 16])
+    a, h, z = (rng.standard_normal(R).astype(np.float32).astype(np.float64) for _ in range(3))
+
+    def loss(l):
+        r = reference(l, t, 0)
+        return (a * r["logprob"] + h * r["entropy"] + z * (r["row_max"] + r["log_sum"])).sum()
+
+    num = np.zeros_like(l)
+    e = 1e-5
+    for i in np.ndindex(l.shape):
+        p, q = l.copy(), l.copy()
+        p[i] += e
+        q[i] -= e
+        num[i] = (loss(p) - loss(q)) / (2 * e)
+    g = dart.token_logprobs_grad(tensor(l), ids(t), tensor(a), dentropy=tensor(h), dlse=tensor(z))
+    assert np.abs(f64(g["dlogits"]) - num).max() <= 1e-5
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 logits: the last rows are what a tensor of their own gives."""
+    import torch
+    V, R = 65536, 33000
+    print("\n[gpu-case] logprobs %d x %d bf16 (%.1f GiB)" % (R, V, R * V * 2 / 2 ** 30), flush=True)
+    l = torch.zeros((R, V), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    l[-3:] = torch.randn((3, V), generator=g, device="cuda").to(torch.bfloat16)
+    t = torch.zeros(R, dtype=torch.int64, device="cuda")
+    t[-3:] = torch.tensor([5, 60000, 65535], device="cuda")
+    dlp = torch.ones(R, device="cuda")
+    small = dart.token_logprobs_grad(l[-3:].clone(), t[-3:].clone(), dlp[-3:].clone(), top_k=3)
+    big = dart.token_logprobs(l, t, top_k=3)
+    for k in ("logprob", "entropy", "row_max", "log_sum", "top_logprobs"):
+        assert torch.allclose(big[k][-3:], small[k], rtol=1e-5, atol=1e-5), k
+    assert big["top_ids"][-3:].equal(small["top_ids"])
+    assert abs(float(big["log_sum"][0]) - np.log(V)) < 1e-5
+    one = dart.token_logprobs_grad(l, t, dlp, dlogits=l)   # in place
+    assert float((one["dlogits"][-3:].float() - small["dlogits"].float()).abs().max()) <= 2 ** -8
+    assert abs(float(one["dlogits"][0, 0]) - (1 - 1 / V)) <= 2 ** -8
+
+
+def test_other_stream_and_refusals():
+    import torch
+    rng = np.random.default_rng(1)
+    l = tensor(rng.standard_normal((3, 150000)), "bf16")
+    t = ids(rng.integers(0, 150000, 3))
+    ref = dart.token_logprobs(l, t, top_k=20)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        r = dart.token_logprobs(l, t, top_k=20, stream=side)
+        junk = [torch.full((1 << 16,), 3.0, device="cuda") for _ in range(8)]
+    side.synchronize()
+    assert all(r[k].equal(ref[k]) for k in ref) and junk
+    with pytest.raises(ValueError):
+        dart.token_logprobs(l, t[:2])
+    with pytest.raises(ValueError):
+        dart.token_logprobs(l, t.int())
+    with pytest.raises(dart.DartError):
+        dart.token_logprobs(l, t, top_k=33)
+    with pytest.raises(dart.DartError):
+        dart.token_logprobs(l[:, :5], t, top_k=6)
+    with pytest.raises(dart.DartError):
+        dart.token_logprobs_bwd(l, ref["row_max"], ref["log_sum"], targets=t, dlogprob=ref["logprob"], dlogits=l.float().view(-1)[:450000].view(3, 150000).to(torch.bfloat16), dentropy=ref["entropy"])
+    with pytest.raises(TypeError):
+        dart.token_logprobs(l.half(), t)
+    with pytest.raises(dart.DartError):
+        dart.token_logprobs_grad(l.float(), t, ref["logprob"], grad_dtype=torch.bfloat16)
