@@ -355,8 +355,7 @@ dart_status dart_gated_rmsnorm_bwd(int64_t rows, int32_t dim, int32_t group, int
  *            residual is
  * out or sum may be x or residual itself (the same pointer, row stride dim);
  * any other overlap of an output is refused.  dim <= 16384, eps > 0.  Any
- * alignment and stride of whole elements; rows that all lie on 16 bytes are
- * faster.
+ * alignment and stride of whole elements.
  */
 dart_status dart_layernorm(int64_t rows, int32_t dim, int32_t dtype, int32_t center, const void* x,
                            int64_t x_row_stride, const void* residual, int64_t residual_row_stride,

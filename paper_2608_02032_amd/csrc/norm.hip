@@ -8,105 +8,449 @@
 //   dw = sum_rows dout (.) xh,  db = sum_rows dout.
 // The mean square is taken of the deviations, never as a difference of
 // squares, which would lose what a large mean leaves.
+//
+// Both are bound by HBM: some ten operations per element against two to eight
+// bytes.  A row stays in the registers of the TPR lanes that share it (16, a
+// wave, four to sixteen waves, ITEMS vectors of V elements each), so every
+// input is read once; the next row's loads are issued ahead of the present
+// row's sums, and a lane keeps its columns' weights for all its rows.  In the
+// backward it keeps their sums of dw and db too: one partial row per
+// workgroup, added in a second launch in a fixed order.
 #include "dart_common.hpp"
 #include "dart_internal.hpp"
 
 namespace dart {
 namespace {
 
-__device__ __forceinline__ float block_sum(float v, float* s_red) {
+// V elements of T as they are loaded and stored: 16 bytes of the wider type of a
+// kernel at any alignment of an element (a lane's 16 bytes are one access
+// whether they lie on 16 or not), or single elements in rows shorter than that.
+typedef unsigned int u32x2_nt __attribute__((ext_vector_type(2)));
+template <typename T, int V> struct Raw;
+template <> struct Raw<bf16, 8> { using type = u32x4_nt; typedef u32x4_nt mem __attribute__((aligned(2))); };
+template <> struct Raw<bf16, 4> { using type = u32x2_nt; typedef u32x2_nt mem __attribute__((aligned(2))); };
+template <> struct Raw<bf16, 1> { using type = uint32_t; typedef uint16_t mem; };
+template <> struct Raw<float, 4> { using type = f32x4; typedef f32x4 mem __attribute__((aligned(4))); };
+template <> struct Raw<float, 1> { using type = float; typedef float mem; };
+template <typename T, int V> using RawT = typename Raw<T, V>::type;
+
+template <typename T, int V>
+__device__ __forceinline__ RawT<T, V> load_raw(const T* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const typename Raw<T, V>::mem*>(p));
+}
+__device__ __forceinline__ float bits_f(uint32_t u) { return __builtin_bit_cast(float, u); }
+__device__ __forceinline__ void unpack(u32x4_nt r, float (&v)[8]) {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-    const int wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_red[wave] = v;
-    __syncthreads();
-    float s = 0.f;
-    for (int i = 0; i < nw; ++i) s += s_red[i];
-    return s;
-}
-
-// One block per row, which it reads once from memory and then from cache.
-template <typename T>
-__global__ __launch_bounds__(256) void k_layernorm(const T* x, int64_t xs, const T* res, int64_t rs,
-                                                   const float* __restrict__ w,
-                                                   const float* __restrict__ b, float eps, T* out,
-                                                   T* sum, int64_t rows, int D, int center) {
-    extern __shared__ float s_row[];
-    __shared__ float s_red[4];
-    const int64_t r = flat_block();
-    if (r >= rows) return;
-    float a = 0.f;
-    for (int i = threadIdx.x; i < D; i += 256) {
-        float v = to_f(x[r * xs + i]);
-        if (res) v = to_f(from_f<T>(v + to_f(res[r * rs + i])));
-        s_row[i] = v;
-        a += v;
-    }
-    const float mu = center ? block_sum(a, s_red) / D : 0.f;
-    float q = 0.f;
-    for (int i = threadIdx.x; i < D; i += 256) q += (s_row[i] - mu) * (s_row[i] - mu);
-    const float inv = 1.0f / sqrtf(block_sum(q, s_red) / D + eps);
-    for (int i = threadIdx.x; i < D; i += 256) {
-        const float v = s_row[i];
-        out[r * D + i] = from_f<T>((v - mu) * inv * (w ? w[i] : 1.f) + (b ? b[i] : 0.f));
-        if (sum) sum[r * D + i] = from_f<T>(v);
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bits_f(r[i] << 16);
+        v[2 * i + 1] = bits_f(r[i] & 0xFFFF0000u);
     }
 }
+__device__ __forceinline__ void unpack(u32x2_nt r, float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[2 * i] = bits_f(r[i] << 16);
+        v[2 * i + 1] = bits_f(r[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void unpack(uint32_t r, float (&v)[1]) { v[0] = bits_f(r << 16); }
+__device__ __forceinline__ void unpack(f32x4 r, float (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = r[i];
+}
+__device__ __forceinline__ void unpack(float r, float (&v)[1]) { v[0] = r; }
+template <int V>
+__device__ __forceinline__ void store_v(bf16* p, const float (&v)[V]) {
+    if constexpr (V == 1) {
+        *p = (bf16)v[0];
+    } else {
+        typedef bf16 vec __attribute__((ext_vector_type(V)));
+        vec r;
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = (bf16)v[i];
+        *reinterpret_cast<typename Raw<bf16, V>::mem*>(p) = __builtin_bit_cast(RawT<bf16, V>, r);
+    }
+}
+template <int V>
+__device__ __forceinline__ void store_v(float* p, const float (&v)[V]) {
+    if constexpr (V == 1) *p = v[0];
+    else *reinterpret_cast<Raw<float, 4>::mem*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+}
 
-// One block per run of rows; the sums of the weight's and the bias's gradient
-// over the run stand in the block's partial row, each column with one thread.
-constexpr int kNormBwdRows = 32;
-template <typename T, typename GT>
-__global__ __launch_bounds__(256) void k_layernorm_bwd(const T* __restrict__ x, int64_t xs,
-                                                       const float* __restrict__ w, float eps,
-                                                       const GT* dout, const GT* dsum, GT* dx,
-                                                       float* __restrict__ part, int64_t rows, int D,
-                                                       int center) {
-    __shared__ float s_red[4];
-    const int64_t blk = flat_block();
-    const int64_t r0 = blk * kNormBwdRows;
-    if (r0 >= rows) return;
-    const int64_t r1 = r0 + kNormBwdRows < rows ? r0 + kNormBwdRows : rows;
-    float* acc = part + blk * 2 * D;
-    for (int64_t r = r0; r < r1; ++r) {
-        float a = 0.f;
-        for (int i = threadIdx.x; i < D; i += 256) a += to_f(x[r * xs + i]);
-        const float mu = center ? block_sum(a, s_red) / D : 0.f;
-        float q = 0.f, g1 = 0.f, g2 = 0.f;
-        for (int i = threadIdx.x; i < D; i += 256) {
-            const float d = to_f(x[r * xs + i]) - mu, g = to_f(dout[r * D + i]) * (w ? w[i] : 1.f);
-            q += d * d;
-            g1 += g;
-            g2 += g * d;
-        }
-        const float inv = 1.0f / sqrtf(block_sum(q, s_red) / D + eps);
-        const float m1 = center ? block_sum(g1, s_red) / D : 0.f, m2 = block_sum(g2, s_red) * inv / D;
-        for (int i = threadIdx.x; i < D; i += 256) {
-            const float xh = (to_f(x[r * xs + i]) - mu) * inv, go = to_f(dout[r * D + i]);
-            const float g = go * (w ? w[i] : 1.f);
-            const float d = inv * (g - m1 - xh * m2) + (dsum ? to_f(dsum[r * D + i]) : 0.f);
-            dx[r * D + i] = from_f<GT>(d);
-            acc[i] = r == r0 ? go * xh : acc[i] + go * xh;
-            acc[D + i] = r == r0 ? go : acc[D + i] + go;
+// Which elements of its vector q a lane owns.  In rows that are no multiple of
+// V elements (RAGGED) the last vector is moved back to end with the row; what
+// it shares with the one before belongs to that one (both store the same).
+template <int V, int TPR, int ITEMS, bool RAGGED>
+struct Columns {
+    int first[ITEMS];  // first column; lanes past the row repeat its last vector
+    int skip[ITEMS];   // elements that are not the lane's own, from the front
+    __device__ __forceinline__ Columns(int lane, int D) {
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            const int c = (lane + q * TPR) * V;
+            first[q] = c <= D - V ? c : D - V;
+            skip[q] = c < D ? c - first[q] : V;
         }
     }
+    __device__ __forceinline__ bool any(int q) const { return skip[q] < V; }
+    __device__ __forceinline__ bool own(int q, int i) const { return RAGGED ? i >= skip[q] : skip[q] == 0; }
+};
+
+// Sums of N values over the TPR lanes of a row, in every one of them.  Rows of
+// several waves meet in LDS; `turn` alternates its halves, so that one barrier
+// per exchange keeps a write from the reads two exchanges before.
+template <int N, int TPR>
+struct RowSum {
+    static constexpr int kWaves = TPR / 64;
+    float (*s)[2][kWaves > 0 ? kWaves : 1];
+    int turn;
+    template <int M>
+    __device__ __forceinline__ void operator()(float (&v)[M]) {
+        static_assert(M <= N, "room for the exchange");
+#pragma unroll
+        for (int k = 0; k < M; ++k) {
+#pragma unroll
+            for (int o = (TPR < 64 ? TPR : 64) / 2; o >= 1; o >>= 1) v[k] += __shfl_xor(v[k], o, 64);
+        }
+        if constexpr (TPR > 64) {
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int k = 0; k < M; ++k) s[k][turn][threadIdx.x >> 6] = v[k];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < M; ++k) {
+                v[k] = 0.f;
+#pragma unroll
+                for (int i = 0; i < kWaves; ++i) v[k] += s[k][turn][i];
+            }
+            turn ^= 1;
+        }
+    }
+};
+
+constexpr int block_threads(int tpr) { return tpr > 256 ? tpr : 256; }
+
+// The row of a workgroup's rows at a time that a lane works on, as a scalar where
+// its whole wave shares it.
+template <int TPR>
+__device__ __forceinline__ int row_group() {
+    if constexpr (TPR >= 256) return 0;
+    else if constexpr (TPR == 64) return __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    else return (int)threadIdx.x / TPR;
 }
 
-int64_t bwd_blocks(int64_t rows) { return (rows + kNormBwdRows - 1) / kNormBwdRows; }
-
-template <typename T>
-void run_layernorm(int64_t rows, int D, int center, const void* x, int64_t xs, const void* res, int64_t rs,
-                   const float* w, const float* b, float eps, void* out, void* sum, hipStream_t st) {
-    k_layernorm<T><<<flat_grid(rows, 256), 256, D * sizeof(float), st>>>(
-        (const T*)x, xs, (const T*)res, rs, w, b, eps, (T*)out, (T*)sum, rows, D, center);
+// Weights of V columns, or `none` where there are none.  A lane keeps those of its
+// columns for all its rows, except where 1024 lanes leave it 128 registers and
+// more than 8 elements each: it loads them again for every row there, and loads
+// no row ahead.
+constexpr bool keeps_weights(int tpr, int e) { return tpr < 1024 || e <= 8; }
+template <int V>
+__device__ __forceinline__ void load_cols(const float* w, int c, float none, float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = w ? w[c + i] : none;
 }
 
-template <typename T, typename GT>
-void run_layernorm_bwd(int64_t rows, int D, int center, const void* x, int64_t xs, const float* w, float eps,
-                       const void* dout, const void* dsum, void* dx, float* part, hipStream_t st) {
-    k_layernorm_bwd<T, GT><<<flat_grid(bwd_blocks(rows), 256), 256, 0, st>>>(
-        (const T*)x, xs, w, eps, (const GT*)dout, (const GT*)dsum, (GT*)dx, part, rows, D, center);
+struct NormArgs {
+    const void *x, *res;
+    int64_t xs, rs, rows;
+    const float *w, *b;
+    float eps, inv_d;
+    void *out, *sum;
+    int D, center;
+};
+
+template <typename T, int V, int TPR, int ITEMS, bool RAGGED>
+__global__ __launch_bounds__(block_threads(TPR)) void k_layernorm(const NormArgs a) {
+    constexpr int GR = block_threads(TPR) / TPR;  // rows at a time
+    __shared__ float s_sum[1][2][TPR > 64 ? TPR / 64 : 1];
+    const int lane = threadIdx.x % TPR, group = row_group<TPR>();
+    const T* x = (const T*)a.x;
+    const T* res = (const T*)a.res;
+    RowSum<1, TPR> row_sum{s_sum, 0};
+    constexpr bool keep = keeps_weights(TPR, ITEMS * V), ahead = keep;
+    float wv[keep ? ITEMS : 1][V], bv[keep ? ITEMS : 1][V];
+    const Columns<V, TPR, ITEMS, RAGGED> cols(lane, a.D);
+#pragma unroll
+    for (int q = 0; q < ITEMS; ++q) {
+        if constexpr (keep) {
+            load_cols(a.w, cols.first[q], 1.f, wv[q]);
+            load_cols(a.b, cols.first[q], 0.f, bv[q]);
+        }
+    }
+    RawT<T, V> xr[ITEMS] = {}, rr[ITEMS] = {};
+    const auto load = [&](int64_t r) {
+        const int64_t rc = r < a.rows ? r : a.rows - 1;
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            xr[q] = load_raw<T, V>(x + rc * a.xs + cols.first[q]);
+            if (res) rr[q] = load_raw<T, V>(res + rc * a.rs + cols.first[q]);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * GR;
+    int64_t base = (int64_t)blockIdx.x * GR;
+    if constexpr (ahead) load(base + group);
+    for (; base < a.rows; base += step) {
+        const int64_t r = base + group;
+        if constexpr (!ahead) load(r);
+        float v[ITEMS][V], m[1] = {0.f};
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            unpack(xr[q], v[q]);
+            if (res) {
+                float u[V];
+                unpack(rr[q], u);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[q][i] = to_f(from_f<T>(v[q][i] + u[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) m[0] += cols.own(q, i) ? v[q][i] : 0.f;
+        }
+        if constexpr (ahead) load(r + step);
+        float mu = 0.f, ss[1] = {0.f};
+        if (a.center) {
+            row_sum(m);
+            mu = m[0] * a.inv_d;
+        }
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) ss[0] += cols.own(q, i) ? (v[q][i] - mu) * (v[q][i] - mu) : 0.f;
+        }
+        row_sum(ss);
+        const float inv = 1.0f / sqrtf(ss[0] * a.inv_d + a.eps);
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            if (cols.any(q) && r < a.rows) {
+                const int64_t at = r * a.D + cols.first[q];
+                if constexpr (!keep) {
+                    load_cols(a.w, cols.first[q], 1.f, wv[0]);
+                    load_cols(a.b, cols.first[q], 0.f, bv[0]);
+                }
+                if (a.sum) store_v((T*)a.sum + at, v[q]);
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = (v[q][i] - mu) * inv * wv[keep ? q : 0][i] + bv[keep ? q : 0][i];
+                store_v((T*)a.out + at, o);
+            }
+        }
+    }
+}
+
+struct NormBwdArgs {
+    const void* x;
+    int64_t xs, rows;
+    const float* w;
+    float eps, inv_d;
+    const void *dout, *dsum;
+    void* dx;
+    float* part;  // [blocks][2][D]
+    int D, center;
+};
+
+template <typename T, typename GT, int V, int TPR, int ITEMS, bool RAGGED>
+__global__ __launch_bounds__(block_threads(TPR)) void k_layernorm_bwd(const NormBwdArgs a) {
+    constexpr int GR = block_threads(TPR) / TPR;
+    constexpr int W = TPR * ITEMS * V;  // columns, with those past the row
+    __shared__ float s_sum[3][2][TPR > 64 ? TPR / 64 : 1];
+    __shared__ float s_col[GR > 1 ? (GR - 1) * W : 1];
+    const int lane = threadIdx.x % TPR, group = row_group<TPR>();
+    const T* x = (const T*)a.x;
+    const GT* dout = (const GT*)a.dout;
+    const GT* dsum = (const GT*)a.dsum;
+    RowSum<3, TPR> row_sum{s_sum, 0};
+    constexpr bool keep = keeps_weights(TPR, ITEMS * V), ahead = keep;
+    float wv[keep ? ITEMS : 1][V], aw[ITEMS][V], ab[ITEMS][V];
+    const Columns<V, TPR, ITEMS, RAGGED> cols(lane, a.D);
+#pragma unroll
+    for (int q = 0; q < ITEMS; ++q) {
+        if constexpr (keep) load_cols(a.w, cols.first[q], 1.f, wv[q]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) aw[q][i] = ab[q][i] = 0.f;
+    }
+    RawT<T, V> xr[ITEMS] = {};
+    RawT<GT, V> dr[ITEMS] = {}, sr[ITEMS] = {};
+    const auto load = [&](int64_t r) {
+        const int64_t rc = r < a.rows ? r : a.rows - 1;
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            xr[q] = load_raw<T, V>(x + rc * a.xs + cols.first[q]);
+            dr[q] = load_raw<GT, V>(dout + rc * a.D + cols.first[q]);
+            if (dsum) sr[q] = load_raw<GT, V>(dsum + rc * a.D + cols.first[q]);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * GR;
+    int64_t base = (int64_t)blockIdx.x * GR;
+    if constexpr (ahead) load(base + group);
+    for (; base < a.rows; base += step) {
+        const int64_t r = base + group;
+        if constexpr (!ahead) load(r);
+        float v[ITEMS][V], m[1] = {0.f};
+        // (the gradients stay packed: a row of theirs in float would cost resident waves)
+        RawT<GT, V> dc[ITEMS], sc[ITEMS];
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            unpack(xr[q], v[q]);
+            dc[q] = dr[q];
+            sc[q] = sr[q];
+#pragma unroll
+            for (int i = 0; i < V; ++i) m[0] += cols.own(q, i) ? v[q][i] : 0.f;
+        }
+        if constexpr (ahead) load(r + step);
+        if (a.center) {
+            row_sum(m);
+            const float mu = m[0] * a.inv_d;
+#pragma unroll
+            for (int q = 0; q < ITEMS; ++q) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[q][i] -= mu;
+            }
+        }
+        float t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            float d[V];
+            unpack(dc[q], d);
+            if constexpr (!keep) load_cols(a.w, cols.first[q], 1.f, wv[0]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float g = d[i] * wv[keep ? q : 0][i];
+                t[0] += cols.own(q, i) ? v[q][i] * v[q][i] : 0.f;
+                t[1] += cols.own(q, i) ? g * v[q][i] : 0.f;
+                t[2] += cols.own(q, i) ? g : 0.f;
+            }
+        }
+        row_sum(t);
+        const float inv = 1.0f / sqrtf(t[0] * a.inv_d + a.eps);
+        const float m1 = a.center ? t[2] * a.inv_d : 0.f, m2 = t[1] * a.inv_d * inv;
+        if (r < a.rows) {
+#pragma unroll
+            for (int q = 0; q < ITEMS; ++q) {
+                float o[V], d[V], e[V];
+                unpack(dc[q], d);
+                unpack(sc[q], e);
+                if constexpr (!keep) load_cols(a.w, cols.first[q], 1.f, wv[0]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float xh = v[q][i] * inv;
+                    o[i] = inv * (d[i] * wv[keep ? q : 0][i] - m1 - xh * m2) + (dsum ? e[i] : 0.f);
+                    aw[q][i] += d[i] * xh;
+                    ab[q][i] += d[i];
+                }
+                if (cols.any(q)) store_v((GT*)a.dx + r * a.D + cols.first[q], o);
+            }
+        }
+    }
+    // the groups' column sums in the order of the groups
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.D;
+    const auto finish = [&](float (&acc)[ITEMS][V], float* out) {
+        if constexpr (GR > 1) {
+            __syncthreads();
+            if (group > 0) {
+#pragma unroll
+                for (int q = 0; q < ITEMS; ++q)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) s_col[(group - 1) * W + (i * ITEMS + q) * TPR + lane] = acc[q][i];
+            }
+            __syncthreads();
+        }
+        if (group > 0) return;
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            for (int k = 0; k + 1 < GR; ++k) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[q][i] += s_col[k * W + (i * ITEMS + q) * TPR + lane];
+            }
+            const int c = cols.first[q];
+            if constexpr (RAGGED || V == 1) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if (cols.own(q, i)) out[c + i] = acc[q][i];
+                }
+            } else if (cols.any(q)) {
+#pragma unroll
+                for (int i = 0; i < V; i += 4) {
+                    const float o[4] = {acc[q][i], acc[q][i + 1], acc[q][i + 2], acc[q][i + 3]};
+                    store4(out + c + i, o);
+                }
+            }
+        }
+    };
+    finish(aw, part);
+    finish(ab, part + a.D);
+}
+
+// Waves a CU holds of a form that keeps E elements per lane (by its registers): the
+// grid is that, and a workgroup walks the rows.  More workgroups than that read
+// the weights again and leave a last round that is not full (16384 rows of 4096
+// bf16 with residual: forward 512 workgroups 80 us, 6.7 TB/s, 1024 85, one per
+// row 285; 32768 rows of 768 backward 768 workgroups 38 us, 5.3 TB/s, 512 44, 1024 47).
+constexpr int waves_per_cu(bool bwd, int v, int e) {
+    return e <= 8 ? 16 : e <= 12 || (e == 16 && (v == 8 || !bwd)) ? 12 : 8;
+}
+template <int TPR, int ITEMS, int V>
+unsigned blocks_for(bool bwd, int64_t rows) {
+    constexpr int threads = block_threads(TPR), waves = threads / 64;
+    const int64_t b = (rows + threads / TPR - 1) / (threads / TPR);
+    const int per = waves_per_cu(bwd, V, ITEMS * V) / waves;
+    const int64_t cap = (int64_t)device_cu_count() * (per > 0 ? per : 1);
+    return (unsigned)(b < cap ? b : cap);
+}
+// Most workgroups of any form of the backward: each leaves a partial row.
+int64_t bwd_cap() { return (int64_t)device_cu_count() * 4; }
+
+// The form that holds a row of n vectors: few idle lanes, few lanes to exchange
+// sums between, and at most 16 elements per lane (beyond that too few waves are
+// resident).  Rows of more than 8192 spill registers in the backward, of 16384
+// bf16 at 2.2 TB/s against 5.4 of 4096.  Rows that are no multiple of a vector, at
+// any alignment: 16384 rows of 4095 bf16 forward 5.0 TB/s, of 4096 6.7 (element by
+// element 1.5).
+#define DART_NORM_FORMS(V, F)                                        \
+    if constexpr (V == 8) {                                          \
+        if (n <= 16) F(8, 16, 1);                                    \
+        else if (n <= 64) F(8, 64, 1);                               \
+        else if (n <= 128) F(8, 64, 2);                              \
+        else if (n <= 256) F(8, 256, 1);                             \
+        else if (n <= 512) F(8, 512, 1);                             \
+        else if (n <= 1024) F(8, 1024, 1);                           \
+        else F(8, 1024, 2);                                          \
+    } else if constexpr (V == 4) {                                   \
+        if (n <= 16) F(4, 16, 1);                                    \
+        else if (n <= 64) F(4, 64, 1);                               \
+        else if (n <= 128) F(4, 64, 2);                              \
+        else if (n <= 192) F(4, 64, 3);                              \
+        else if (n <= 256) F(4, 256, 1);                             \
+        else if (n <= 512) F(4, 256, 2);                             \
+        else if (n <= 1024) F(4, 512, 2);                            \
+        else if (n <= 2048) F(4, 1024, 2);                           \
+        else F(4, 1024, 4);                                          \
+    } else {                                                         \
+        F(1, 16, 1); /* rows of less than one vector */              \
+    }
+
+template <typename T, int V>
+void run_layernorm(const NormArgs& a, hipStream_t st) {
+    const int n = (a.D + V - 1) / V;
+#define DART_F(V_, TPR, ITEMS)                                                                                          \
+    a.D % V_ == 0                                                                                                       \
+        ? k_layernorm<T, V_, TPR, ITEMS, false><<<blocks_for<TPR, ITEMS, V_>(false, a.rows), block_threads(TPR), 0, st>>>(a) \
+        : k_layernorm<T, V_, TPR, ITEMS, true><<<blocks_for<TPR, ITEMS, V_>(false, a.rows), block_threads(TPR), 0, st>>>(a)
+    DART_NORM_FORMS(V, DART_F)
+#undef DART_F
+}
+
+// Returns the number of partial rows.
+template <typename T, typename GT, int V>
+unsigned run_layernorm_bwd(const NormBwdArgs& a, hipStream_t st) {
+    const int n = (a.D + V - 1) / V;
+    unsigned blocks = 0;
+#define DART_F(V_, TPR, ITEMS)                                                                        \
+    (blocks = blocks_for<TPR, ITEMS, V_>(true, a.rows),                                               \
+     a.D % V_ == 0 ? k_layernorm_bwd<T, GT, V_, TPR, ITEMS, false><<<blocks, block_threads(TPR), 0, st>>>(a) \
+                   : k_layernorm_bwd<T, GT, V_, TPR, ITEMS, true><<<blocks, block_threads(TPR), 0, st>>>(a))
+    DART_NORM_FORMS(V, DART_F)
+#undef DART_F
+    return blocks;
 }
 
 }  // namespace
@@ -115,15 +459,18 @@ hipError_t launch_layernorm(int dtype, int64_t rows, int D, int center, const vo
                             const void* res, int64_t rs, const float* w, const float* b, float eps,
                             void* out, void* sum, hipStream_t st) {
     if (rows == 0) return hipSuccess;
+    const NormArgs a{x, res, xs, rs, rows, w, b, eps, 1.0f / D, out, sum, D, center};
+    const bool wide = D >= (dtype == 1 ? 8 : 4);
     prof_begin("k_layernorm", st);
-    if (dtype == 1) run_layernorm<bf16>(rows, D, center, x, xs, res, rs, w, b, eps, out, sum, st);
-    else run_layernorm<float>(rows, D, center, x, xs, res, rs, w, b, eps, out, sum, st);
+    if (dtype == 1) wide ? run_layernorm<bf16, 8>(a, st) : run_layernorm<bf16, 1>(a, st);
+    else wide ? run_layernorm<float, 4>(a, st) : run_layernorm<float, 1>(a, st);
     prof_end(st);
     return hipGetLastError();
 }
 
 size_t layernorm_bwd_workspace_bytes(int64_t rows, int D) {
-    return align256(sizeof(float) * (size_t)bwd_blocks(rows) * 2 * D);
+    const int64_t cap = bwd_cap();
+    return align256(sizeof(float) * (size_t)(rows < cap ? rows : cap) * 2 * D);
 }
 
 hipError_t launch_layernorm_bwd(int dtype, int gdtype, int64_t rows, int D, int center, const void* x,
@@ -131,12 +478,17 @@ hipError_t launch_layernorm_bwd(int dtype, int gdtype, int64_t rows, int D, int 
                                 const void* dsum, void* dx, float* dw, float* db, void* ws,
                                 hipStream_t st) {
     float* part = reinterpret_cast<float*>(ws);
-    const int64_t nb = bwd_blocks(rows);
+    unsigned nb = 0;
     if (rows > 0) {
+        const NormBwdArgs a{x, xs, rows, w, eps, 1.0f / D, dout, dsum, dx, part, D, center};
+        const bool wide = D >= (gdtype == 1 ? 8 : 4);
         prof_begin("k_layernorm_bwd", st);
-        if (dtype == 0) run_layernorm_bwd<float, float>(rows, D, center, x, xs, w, eps, dout, dsum, dx, part, st);
-        else if (gdtype == 0) run_layernorm_bwd<bf16, float>(rows, D, center, x, xs, w, eps, dout, dsum, dx, part, st);
-        else run_layernorm_bwd<bf16, bf16>(rows, D, center, x, xs, w, eps, dout, dsum, dx, part, st);
+        if (dtype == 0)
+            nb = wide ? run_layernorm_bwd<float, float, 4>(a, st) : run_layernorm_bwd<float, float, 1>(a, st);
+        else if (gdtype == 0)
+            nb = wide ? run_layernorm_bwd<bf16, float, 4>(a, st) : run_layernorm_bwd<bf16, float, 1>(a, st);
+        else
+            nb = wide ? run_layernorm_bwd<bf16, bf16, 8>(a, st) : run_layernorm_bwd<bf16, bf16, 1>(a, st);
         prof_end(st);
     }
     // a partial row is one item of 2 D values: the first D are the weight's sums
