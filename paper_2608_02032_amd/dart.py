@@ -6,7 +6,6 @@ library has not been built, every call raises -- there is no fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -550,25 +549,42 @@ def _one_device(*tensors):
     """The tensors' device, which has to be one GPU, the current one: the
     library launches on the current device's streams."""
     torch = _torch()
-    device = None
+    index = None
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        i = t.get_device()
+        if i < 0:
             raise ValueError("tensor must live on the GPU")
-        if device is None:
-            device = t.device
-        elif t.device != device:
-            raise ValueError("tensors live on %s and %s" % (device, t.device))
-    if device is not None and device.index != torch.cuda.current_device():
-        raise ValueError("tensors live on %s, which is not the current device" % (device,))
-    return device
+        if index is None:
+            index, first = i, t
+        elif i != index:
+            raise ValueError("tensors live on cuda:%d and cuda:%d" % (index, i))
+    if index is None:
+        return None
+    if index != torch.cuda.current_device():
+        raise ValueError("tensors live on cuda:%d, which is not the current device" % index)
+    return first.device
 
 
-def _allocating(stream):
-    """What is allocated for a call on another stream belongs to that stream's
-    memory, so that it is not handed on while the call still uses it."""
-    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+def _allocator(stream):
+    """torch.empty; for a call on another stream in that stream's memory, so
+    that it is not handed on while the call still uses it."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty
+
+    def empty(*args, **kw):
+        with torch.cuda.stream(stream):
+            return torch.empty(*args, **kw)
+    return empty
+
+
+def _like(t, stream):
+    """A contiguous tensor of t's shape and type."""
+    if stream is None and t.is_contiguous():
+        return _torch().empty_like(t)
+    return _allocator(stream)(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _row_stride(t, name) -> int:
@@ -593,7 +609,7 @@ def _row_stride(t, name) -> int:
 def _same(t, shape, dtype, name, contiguous=True):
     if t is None:
         return
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError("%s must be a %s tensor of shape %s" % (name, dtype, tuple(shape)))
     if contiguous and not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
@@ -614,7 +630,7 @@ def layernorm(x, weight=None, bias=None, residual=None, eps=DEFAULT_EPS, center=
     torch = _torch()
     lib = load_library()
     dtype = _dtype_num(x)
-    device = _one_device(x, weight, bias, residual, out, sum_out)
+    _one_device(x, weight, bias, residual, out, sum_out)
     D = x.shape[-1]
     rows = x.numel() // D if D else 0
     f32 = torch.float32
@@ -627,11 +643,10 @@ def layernorm(x, weight=None, bias=None, residual=None, eps=DEFAULT_EPS, center=
         raise ValueError("sum_out needs a residual")
     xs = _row_stride(x, "x")
     rs = D if residual is None else _row_stride(residual, "residual")
-    with _allocating(stream):
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=device)
-        if residual is not None and sum_out is None:
-            sum_out = torch.empty(x.shape, dtype=x.dtype, device=device)
+    if out is None:
+        out = _like(x, stream)
+    if residual is not None and sum_out is None:
+        sum_out = _like(x, stream)
     check(lib.dart_layernorm(rows, D, dtype, int(bool(center)), x.data_ptr(), xs, _addr(residual), rs,
                              _addr(weight), _addr(bias), float(eps), out.data_ptr(), _addr(sum_out),
                              _stream(stream)))
@@ -658,15 +673,15 @@ def layernorm_bwd(x, dout, weight=None, dsum=None, eps=DEFAULT_EPS, center=True,
     _same(dsum, x.shape, dout.dtype, "dsum")
     _same(dx, x.shape, dout.dtype, "dx")
     xs = _row_stride(x, "x")
-    with _allocating(stream):
-        if dx is None:
-            dx = torch.empty(x.shape, dtype=dout.dtype, device=device)
-        dw = torch.empty((D,), dtype=torch.float32, device=device) if weight is not None else None
-        db = torch.empty((D,), dtype=torch.float32, device=device) if want_bias else None
-        ws = _workspace(lib.dart_layernorm_bwd_workspace_bytes(rows, D), device)
+    empty = _allocator(stream)
+    if dx is None:
+        dx = _like(dout, stream)
+    dw = empty((D,), dtype=torch.float32, device=device) if weight is not None else None
+    db = empty((D,), dtype=torch.float32, device=device) if want_bias else None
+    ws = empty((max(lib.dart_layernorm_bwd_workspace_bytes(rows, D), 1),), dtype=torch.uint8, device=device)
     check(lib.dart_layernorm_bwd(rows, D, dtype, gdtype, int(bool(center)), x.data_ptr(), xs,
                                  _addr(weight), float(eps), dout.data_ptr(), _addr(dsum),
-                                 dx.data_ptr(), _addr(dw), _addr(db), ws.data_ptr(), ws.numel(),
+                                 dx.data_ptr(), _addr(dw), _addr(db), ws.data_ptr(), ws.shape[0],
                                  _stream(stream)))
     return {"dx": dx, "dweight": dw, "dbias": db}
 
@@ -680,17 +695,16 @@ def _logits_args(logits, targets, *others):
     return device, lead, logits.numel() // V if V else 0, V, _row_stride(logits, "logits")
 
 
-def _dlogits(dlogits, logits, grad_dtype, stride):
+def _dlogits(dlogits, logits, grad_dtype, stride, empty):
     """The gradient's tensor: rows at the stride of the logits', so that their
     alignment is the logits' too."""
-    torch = _torch()
     if dlogits is not None:
         if dlogits.shape != logits.shape:
             raise ValueError("dlogits must have the shape of logits")
         return dlogits, _row_stride(dlogits, "dlogits")
     dtype = logits.dtype if grad_dtype is None else grad_dtype
     V = logits.shape[-1]
-    buf = torch.empty(tuple(logits.shape[:-1]) + (stride,), dtype=dtype, device=logits.device)
+    buf = empty(tuple(logits.shape[:-1]) + (stride,), dtype=dtype, device=logits.device)
     return (buf if stride == V else buf[..., :V]), stride
 
 
@@ -701,31 +715,33 @@ def _token_logprobs(logits, targets, top_k, ignore_index, stream, grad=None):
     device, lead, rows, V, stride = _logits_args(logits, targets, *others)
     dtype = _dtype_num(logits)
     top_k = int(top_k)
-    f32 = dict(dtype=torch.float32, device=device)
     if grad is not None:
         for k in ("dlogprob", "dentropy", "dlse"):
             _same(grad[k], lead, torch.float32, k)
-    with _allocating(stream):
-        r = {"logprob": torch.empty(lead, **f32) if targets is not None else None,
-             "entropy": torch.empty(lead, **f32), "row_max": torch.empty(lead, **f32),
-             "log_sum": torch.empty(lead, **f32), "top_ids": None, "top_logprobs": None}
-        if top_k > 0:
-            r["top_ids"] = torch.empty(lead + (top_k,), dtype=torch.int64, device=device)
-            r["top_logprobs"] = torch.empty(lead + (top_k,), **f32)
-        ws = _workspace(lib.dart_token_logprobs_workspace_bytes(rows, V, dtype, top_k), device)
-        if grad is not None:
-            r["dlogits"], ds = _dlogits(grad["dlogits"], logits, grad["dtype"], stride)
-    fwd = [_addr(r[k]) for k in ("logprob", "entropy", "row_max", "log_sum", "top_ids", "top_logprobs")]
+    empty = _allocator(stream)
+    rows_out = empty((4,) + lead, dtype=torch.float32, device=device)
+    logprob, entropy, row_max, log_sum = rows_out.unbind(0)
+    top_ids = top_logprobs = None
+    if top_k > 0:
+        top_ids = empty(lead + (top_k,), dtype=torch.int64, device=device)
+        top_logprobs = empty(lead + (top_k,), dtype=torch.float32, device=device)
+    need = lib.dart_token_logprobs_workspace_bytes(rows, V, dtype, top_k)
+    ws = empty((need,), dtype=torch.uint8, device=device) if need else None
+    r = {"logprob": logprob if targets is not None else None, "entropy": entropy, "row_max": row_max,
+         "log_sum": log_sum, "top_ids": top_ids, "top_logprobs": top_logprobs}
+    at, n = rows_out.data_ptr(), 4 * rows
+    fwd = (at if targets is not None else None, at + n, at + 2 * n, at + 3 * n, _addr(top_ids),
+           _addr(top_logprobs))
+    if grad is not None:
+        r["dlogits"], ds = _dlogits(grad["dlogits"], logits, grad["dtype"], stride, empty)
     if grad is None:
         check(lib.dart_token_logprobs(rows, V, stride, dtype, logits.data_ptr(), _addr(targets),
-                                      int(ignore_index), top_k, *fwd, ws.data_ptr(), ws.numel(),
-                                      _stream(stream)))
+                                      int(ignore_index), top_k, *fwd, _addr(ws), need, _stream(stream)))
     else:
         check(lib.dart_token_logprobs_grad(
             rows, V, stride, dtype, _dtype_num(r["dlogits"]), logits.data_ptr(), _addr(targets),
             int(ignore_index), top_k, _addr(grad["dlogprob"]), _addr(grad["dentropy"]),
-            _addr(grad["dlse"]), *fwd, r["dlogits"].data_ptr(), ds, ws.data_ptr(), ws.numel(),
-            _stream(stream)))
+            _addr(grad["dlse"]), *fwd, r["dlogits"].data_ptr(), ds, _addr(ws), need, _stream(stream)))
     return r
 
 
@@ -757,8 +773,7 @@ def token_logprobs_bwd(logits, row_max, log_sum, targets=None, dlogprob=None, en
     for t, nm in ((row_max, "row_max"), (log_sum, "log_sum"), (entropy, "entropy"),
                   (dlogprob, "dlogprob"), (dentropy, "dentropy"), (dlse, "dlse")):
         _same(t, lead, torch.float32, nm)
-    with _allocating(stream):
-        dlogits, ds = _dlogits(dlogits, logits, grad_dtype, stride)
+    dlogits, ds = _dlogits(dlogits, logits, grad_dtype, stride, _allocator(stream))
     check(lib.dart_token_logprobs_bwd(rows, V, stride, _dtype_num(logits), _dtype_num(dlogits),
                                       logits.data_ptr(), _addr(targets), int(ignore_index),
                                       row_max.data_ptr(), log_sum.data_ptr(), _addr(entropy),
@@ -790,23 +805,18 @@ def _dense(t) -> bool:
 
 
 def _tensor_list(tensors, name):
-    """(pointers, element counts, types) of a list of dense tensors."""
+    """(pointers, element counts, types) of a list of dense tensors on one device."""
     torch = _torch()
     types = {torch.float32: DART_FP32, torch.bfloat16: DART_BF16}
-    ptrs, numels, dtypes = array("q"), array("q"), array("i")
-    device = tensors[0].device if tensors else None
-    for t in tensors:
-        if t.device != device:
-            raise ValueError("%s live on %s and %s" % (name, device, t.device))
-        code = types.get(t.dtype)
-        if code is None:
-            raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
-        if not t.is_contiguous() and not _dense(t):
-            raise ValueError("%s must be dense (no gaps, no repeated elements)" % name)
-        ptrs.append(t.data_ptr())
-        numels.append(t.numel())
-        dtypes.append(code)
-    return ptrs, numels, dtypes
+    if len({t.get_device() for t in tensors}) > 1:
+        raise ValueError("%s live on different devices" % name)
+    dtypes = [types.get(t.dtype) for t in tensors]
+    if None in dtypes:
+        raise TypeError("%s must be float32 or bfloat16" % name)
+    if not all([t.is_contiguous() or _dense(t) for t in tensors]):
+        raise ValueError("%s must be dense (no gaps, no repeated elements)" % name)
+    return (array("q", [t.data_ptr() for t in tensors]), array("q", [t.numel() for t in tensors]),
+            array("i", dtypes))
 
 
 def _host(a):
@@ -841,19 +851,21 @@ def _clip(grads, out, max_norm, scale, stream):
             raise ValueError("%d outputs for %d gradients" % (len(out), n))
         optrs, onumels, odtypes = _tensor_list(out, "outputs")
         _one_device(*grads[:1], *out[:1])
-        for g, o in zip(grads, out):
-            if g.shape != o.shape or (g.stride() != o.stride() and not (g.is_contiguous() and o.is_contiguous())):
-                raise ValueError("an output must have its gradient's shape and order of elements")
-    with _allocating(stream):
-        norm = torch.empty((), dtype=torch.float32, device=device)
-        ws = _workspace(lib.dart_grad_norm_workspace_bytes(n), device)
+        if [t.shape for t in grads] != [t.shape for t in out] or any(
+                [not (g.is_contiguous() and o.is_contiguous()) and g.stride() != o.stride()
+                 for g, o in zip(grads, out)]):
+            raise ValueError("an output must have its gradient's shape and order of elements")
+    empty = _allocator(stream)
+    norm = empty((), dtype=torch.float32, device=device)
+    need = lib.dart_grad_norm_workspace_bytes(n)
+    ws = empty((need,), dtype=torch.uint8, device=device)
     if out is None:
         check(lib.dart_grad_norm(n, _host(ptrs), _host(numels), _host(dtypes), float(scale),
-                                 norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+                                 norm.data_ptr(), ws.data_ptr(), need, _stream(stream)))
     else:
         check(lib.dart_clip_grad_norm(n, _host(ptrs), _host(optrs), _host(numels), _host(dtypes),
                                       _host(odtypes), max_norm, float(scale), norm.data_ptr(),
-                                      ws.data_ptr(), ws.numel(), _stream(stream)))
+                                      ws.data_ptr(), need, _stream(stream)))
     return norm
 
 
