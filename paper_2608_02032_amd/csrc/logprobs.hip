@@ -93,26 +93,25 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
     const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
     return (uint64_t)hi << 32 | lo;
 }
-__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) {
+template <bool LARGEST>
+__device__ __forceinline__ uint32_t wave_pick_u32(uint32_t v) {
     const auto dpp = [](auto ctrl, uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(ctrl)::value, 0xF, 0xF, false); };
-    const auto lower = [](uint32_t x, uint32_t y) { return x < y ? x : y; };
-    v = lower(v, dpp(std::integral_constant<int, 0xB1>{}, v));
-    v = lower(v, dpp(std::integral_constant<int, 0x4E>{}, v));
-    v = lower(v, dpp(std::integral_constant<int, 0x141>{}, v));
-    v = lower(v, dpp(std::integral_constant<int, 0x140>{}, v));
+    const auto pick = [](uint32_t x, uint32_t y) { return (x < y) == LARGEST ? y : x; };
+    v = pick(v, dpp(std::integral_constant<int, 0xB1>{}, v));
+    v = pick(v, dpp(std::integral_constant<int, 0x4E>{}, v));
+    v = pick(v, dpp(std::integral_constant<int, 0x141>{}, v));
+    v = pick(v, dpp(std::integral_constant<int, 0x140>{}, v));
     uint32_t a = v, b = v;
     asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
-    uint32_t c = lower(a, b), d = c;
+    uint32_t c = pick(a, b), d = c;
     asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(c), "+v"(d));
-    return lower(c, d);
+    return pick(c, d);
 }
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) { return wave_pick_u32<false>(v); }
 __device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const uint64_t w = (uint64_t)__shfl_xor((unsigned long long)v, o, 64);
-        v = w > v ? w : v;
-    }
-    return v;
+    const uint32_t hi = wave_pick_u32<true>((uint32_t)(v >> 32));
+    const uint32_t lo = wave_pick_u32<true>((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0);
+    return (uint64_t)hi << 32 | lo;
 }
 
 // What a row's gradient needs: dl_j = p_j (f + h log p_j) + [j = t] a.
@@ -233,15 +232,27 @@ struct Top<TPR, true> {
             s.count = 0;
         }
     }
-    __device__ __forceinline__ void bound() {
-        if (threadIdx.x >= 64) return;
+    // (by one wave, another for the next row: the first waves of a CU's workgroups
+    // may share a SIMD)
+    __device__ __forceinline__ void bound(int by) {
+        if ((int)(threadIdx.x >> 6) != by) return;
+        const int lane = threadIdx.x & 63;
         uint64_t c = 0;
 #pragma unroll
-        for (int w = 0; w < TPR / 64; ++w) c = s.own[w][threadIdx.x] > c ? s.own[w][threadIdx.x] : c;
-        int above = 0;
+        for (int w = 0; w < TPR / 64; ++w) c = s.own[w][lane] > c ? s.own[w][lane] : c;
+        uint64_t kth = 0;
+        if (k <= 8) {  // the largest k times: 40 instructions each, against 400 to count
+            for (int i = 0; i < k; ++i) {
+                kth = wave_max64(c);
+                if (c == kth) c = 0;
+            }
+        } else {
+            int above = 0;
 #pragma unroll 8
-        for (int j = 0; j < 64; ++j) above += lane_key(c, j) > c;
-        if (above == k - 1 && c > 0) s.bound = c;
+            for (int j = 0; j < 64; ++j) above += lane_key(c, j) > c;
+            if (above == k - 1) kth = c;
+        }
+        if (kth > 0) s.bound = kth;
     }
     __device__ __forceinline__ void push(uint64_t key) {
         const int at = atomicAdd(&s.count, 1);
@@ -249,14 +260,15 @@ struct Top<TPR, true> {
     }
     // emit(place, key) of the k largest; each(f) calls f on every key of the thread.
     template <typename Emit, typename Each>
-    __device__ __forceinline__ void finish(bool pushed, const Emit& emit, const Each& each) {
+    __device__ __forceinline__ void finish(int by, bool pushed, const Emit& emit, const Each& each) {
         const int n = pushed ? s.count : kRoom + 1;
         if (n <= 64) {
-            if (threadIdx.x < 64) {
-                const uint64_t c = (int)threadIdx.x < n ? s.room[threadIdx.x] : 0;
+            if ((int)(threadIdx.x >> 6) == by) {
+                const int lane = threadIdx.x & 63;
+                const uint64_t c = lane < n ? s.room[lane] : 0;
                 int above = 0;
                 for (int j = 0; j < n; ++j) above += lane_key(c, j) > c;
-                if ((int)threadIdx.x < n && above < k) emit(above, c);
+                if (lane < n && above < k) emit(above, c);
             }
         } else if (n <= kRoom) {
             for (int i = threadIdx.x; i < n; i += TPR) {
@@ -363,6 +375,7 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
             }
         }
         Top<TPR, TOP> top(sh, a.top_k);
+        const int by = (int)((uint64_t)item % (TPR / 64));
         const auto edge_key = [&] { return has_edge ? order_key(edge, e0 + (uint32_t)cut.edge(tid)) : 0; };
         // one wave takes few alternatives round by round; by the bound it costs some 1000
         // instructions whatever their number
@@ -382,7 +395,7 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
             for (int w = 0; w < TPR / 64; ++w) m = fmaxf(m, sh.st.m[w]);
         }
         if constexpr (TOP) {
-            if (!by_rounds) top.bound();  // (the first wave; the others go on)
+            if (!by_rounds) top.bound(by);  // (the other waves go on)
         }
         float s = 0.f, c = 0.f;
 #pragma unroll
@@ -471,7 +484,7 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
                         if (tid == 0) emit(k, order_key(last, j));
                     }
                 } else {
-                    top.finish(false, emit, each);
+                    top.finish(by, false, emit, each);
                 }
             } else {
                 const uint64_t bound = sh.top.bound;
@@ -505,7 +518,7 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
                 if constexpr (SEG) {
                     if (tid >= cut.n && tid < a.top_k) sg.top[item * a.top_k + tid] = 0;
                 }
-                top.finish(orderly, emit, each);
+                top.finish(by, orderly, emit, each);
             }
         }
 
@@ -570,7 +583,7 @@ __global__ __launch_bounds__(256) void k_token_logprobs_join(const LogprobArgs a
     if ((tid & 63) == 0) sh.st.m[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(sh.st.m[0], sh.st.m[1]), fmaxf(sh.st.m[2], sh.st.m[3]));
-    if constexpr (TOP) top.bound();
+    if constexpr (TOP) top.bound(0);
     float s = 0.f, c = 0.f;
     for (int i = tid; i < sg.nseg; i += 256) {
         const Part p = part[i];
@@ -593,7 +606,7 @@ __global__ __launch_bounds__(256) void k_token_logprobs_join(const LogprobArgs a
         const uint64_t bound = sh.top.bound;
         if (top.mine >= bound) each([&](uint64_t key) { if (key >= bound) top.push(key); });
         __syncthreads();
-        top.finish(true, [&](int at, uint64_t key) {
+        top.finish(0, true, [&](int at, uint64_t key) {
             a.top_ids[r * a.top_k + at] = key_index(key);
             a.top_logprobs[r * a.top_k + at] = (key_value(key) - row.m) - row.ls;
         }, each);
@@ -662,10 +675,18 @@ struct Plan {
     int nseg, tpr, nv;
     int64_t len;
 };
-Plan plan_for(int64_t rows, int64_t vocab, int dtype, bool grad) {
+Plan plan_for(int64_t rows, int64_t vocab, int dtype, int top_k, bool grad) {
     const int vec = dtype == 1 ? 8 : 4;
     static const int forms[][2] = {{64, 0}, {64, 1}, {64, 2}, {64, 4}, {256, 2}, {256, 4}, {256, 8}, {512, 8}, {512, 13}, {512, 16}, {1024, 16}};
     const int64_t most = 1024 * 16 * vec;
+    // long rows without alternatives or gradient in segments of 256 threads, if those
+    // are nearly full: more of them are resident, and nothing waits for a whole row
+    // (4096 rows of 131072 bf16 194 us, 5.5 TB/s, whole 242; of 50257 float 136 and 160;
+    // but 8192 of 50257 bf16, 0.77 full, 241 and 190, and with five alternatives,
+    // which every segment sorts, 4096 of 131072 322 and 286)
+    const int64_t full = 256 * 8 * vec, parts = (vocab + full - 1) / full;
+    if (!grad && top_k == 0 && parts > 1 && rows * parts >= 2 * device_cu_count() && 8 * vocab >= 7 * parts * full)
+        return {(int)parts, 256, 8, (vocab + parts - 1) / parts};
     // whole rows where they fit and fill the card, or are short
     if (vocab <= 2048 || (vocab <= most && rows >= device_cu_count() / (grad ? 4 : 2))) {
         for (const auto& f : forms)
@@ -724,7 +745,7 @@ void run_bwd(const LogprobArgs& a, const LogprobGrad& g, hipStream_t st) {
 size_t token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int top_k) {
     size_t need = 0;
     for (const bool grad : {false, true}) {
-        const Plan p = plan_for(rows, vocab, dtype, grad);
+        const Plan p = plan_for(rows, vocab, dtype, top_k, grad);
         if (p.nseg > 1) {
             const size_t n = (size_t)rows * p.nseg, b = align256(n * sizeof(Part)) + n * top_k * sizeof(uint64_t);
             need = b > need ? b : need;
@@ -735,7 +756,7 @@ size_t token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int dtype, in
 
 hipError_t launch_token_logprobs(const LogprobArgs& a, const LogprobGrad* grad, void* ws, hipStream_t st) {
     if (a.rows == 0) return hipSuccess;
-    const Plan p = plan_for(a.rows, a.vocab, a.dtype, grad != nullptr);
+    const Plan p = plan_for(a.rows, a.vocab, a.dtype, a.top_k, grad != nullptr);
     SegArgs sg{p.nseg, p.len, nullptr, nullptr};
     const LogprobGrad none{};
     if (p.nseg > 1) {

@@ -3,11 +3,13 @@ paper's App. D.1: two-layer models, chunk size 16, state size N in {16, 64}).
 
 Every step of the DART path -- the width-4 convolution with SiLU, the step
 sizes, the chunked scan with its chunk memories, state-memory attention with
-the gated residual, the gated RMSNorm -- runs forward and backward in the
-library's HIP kernels through the torch.autograd.Function wrappers below;
-PyTorch supplies the plain GEMMs around them (input and output projections,
-embeddings, the LM head), the optimiser and device memory.  The residual-
-stream RMSNorm and the D skip are elementwise torch ops.
+the gated residual, the gated RMSNorm -- and the steps around the blocks --
+the residual stream's RMSNorm, the log probabilities and their gradient, the
+clipping of the gradients -- run forward and backward in the library's HIP
+kernels, the differentiable ones through the torch.autograd.Function wrappers
+below; PyTorch supplies the plain GEMMs around them (input and output
+projections, embeddings, the LM head), the optimiser and device memory.  The
+D skip and the residual addition are elementwise torch ops.
 
 Storage is float32 (the library's fp32 path); the gradients the library
 returns are float32 as well.
@@ -18,7 +20,6 @@ import math
 
 import torch
 import torch.nn as nn
-import torch.nn.functional as F
 
 from . import dart
 
@@ -107,12 +108,81 @@ class _GatedNorm(torch.autograd.Function):
         return g["dy"], g["dz"], g["dweight"]
 
 
+class _Norm(torch.autograd.Function):
+    """RMSNorm(u) w, the norm of the residual stream."""
+
+    @staticmethod
+    def forward(ctx, u, w):
+        u = u.contiguous()
+        ctx.save_for_backward(u, w)
+        return dart.layernorm(u, w, center=False)
+
+    @staticmethod
+    def backward(ctx, dout):
+        u, w = ctx.saved_tensors
+        g = dart.layernorm_bwd(u, dout.contiguous(), w, center=False)
+        return g["dx"], g["dweight"]
+
+
+class _AddNorm(torch.autograd.Function):
+    """(u, d, w) -> (s, RMSNorm(s) w) with s = u + d: what reaches s past the norm
+    joins the norm's own gradient in its kernel."""
+
+    @staticmethod
+    def forward(ctx, u, d, w):
+        out, s = dart.layernorm(u.contiguous(), w, residual=d.contiguous(), center=False)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(s, w)
+        return s, out
+
+    @staticmethod
+    def backward(ctx, ds, dout):
+        s, w = ctx.saved_tensors
+        if dout is None:
+            return ds, ds, None
+        g = dart.layernorm_bwd(s, dout.contiguous(), w, center=False,
+                               dsum=None if ds is None else ds.contiguous())
+        return g["dx"], g["dx"], g["dweight"]
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    """(logits, targets, ignore_index) -> (log probabilities, entropies)."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, ignore_index):
+        r = dart.token_logprobs(logits, targets, ignore_index=ignore_index)
+        ctx.ignore_index = ignore_index
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(logits, targets, r["row_max"], r["log_sum"], r["entropy"])
+        return r["logprob"], r["entropy"]
+
+    @staticmethod
+    def backward(ctx, dlogprob, dentropy):
+        logits, targets, row_max, log_sum, entropy = ctx.saved_tensors
+        dl = dart.token_logprobs_bwd(
+            logits, row_max, log_sum, targets=targets,
+            dlogprob=None if dlogprob is None else dlogprob.contiguous(), entropy=entropy,
+            dentropy=None if dentropy is None else dentropy.contiguous(),
+            ignore_index=ctx.ignore_index)
+        return dl, None, None
+
+
+def add_norm(u, d, w):
+    """(u + d, RMSNorm(u + d) w), differentiable: the residual addition with the
+    norm that follows it (dart.layernorm)."""
+    return _AddNorm.apply(u, d, w)
+
+
+def token_logprobs(logits, targets, ignore_index=-100):
+    """Log probabilities [..] of targets [..] int64 under logits [..][V] (0 where
+    the target is ignore_index) and the entropies [..] of the distributions,
+    differentiable (dart.token_logprobs)."""
+    return _TokenLogprobs.apply(logits, targets.contiguous(), ignore_index)
+
+
 # --------------------------------------------------------------------------- #
 # the block and a small language model
 # --------------------------------------------------------------------------- #
-
-def _rmsnorm(u, w, eps=1e-6):
-    return u * torch.rsqrt(u.pow(2).mean(-1, keepdim=True) + eps) * w
 
 
 class DartBlock(nn.Module):
@@ -149,7 +219,7 @@ class DartBlock(nn.Module):
     def forward(self, u):
         B_, L, _ = u.shape
         H, P, N, G = self.H, self.P, self.N, self.G
-        proj = self.in_proj(_rmsnorm(u, self.norm_w))
+        proj = self.in_proj(_Norm.apply(u, self.norm_w))
         z, xbc, dtr, q, e, g = torch.split(proj, self.splits, dim=-1)
         xbc = _ConvSiLU.apply(xbc.contiguous(), self.conv_w, self.conv_b)
         x, Bm, Cm = torch.split(xbc, [self.d_inner, G * N, G * N], dim=-1)
@@ -181,7 +251,7 @@ class DartLM(nn.Module):
         u = self.emb(tokens)
         for blk in self.blocks:
             u = blk(u)
-        return self.head(_rmsnorm(u, self.norm_w))
+        return self.head(_Norm.apply(u, self.norm_w))
 
 
 def train_mqar(steps, L=256, R=None, batch=64, d_model=64, d_state=16, chunk=16, lr=1e-3,
@@ -206,16 +276,19 @@ def train_mqar(steps, L=256, R=None, batch=64, d_model=64, d_state=16, chunk=16,
         tok = torch.from_numpy(tok).to(device)
         lab = torch.from_numpy(lab).to(device)
         logits = model(tok)
-        loss = F.cross_entropy(logits.view(-1, vocab.size), lab.view(-1), ignore_index=mqar.IGNORE)
-        with torch.no_grad():
-            m = lab != mqar.IGNORE
-            acc = (logits.argmax(-1)[m] == lab[m]).float().mean()
+        # the mean cross entropy over the targets: its gradient with respect to each
+        # log probability is known ahead, so one call gives both
+        m = lab != mqar.IGNORE
+        n = m.sum()
+        r = dart.token_logprobs_grad(logits.detach(), lab, -m.float() / n, top_k=1, ignore_index=mqar.IGNORE)
+        loss = -r["logprob"].sum() / n
+        acc = (r["top_ids"][..., 0] == lab).sum() / n
         opt.zero_grad(set_to_none=True)
-        loss.backward()
-        torch.nn.utils.clip_grad_norm_(model.parameters(), 1.0)
+        logits.backward(r["dlogits"])
+        dart.clip_grad_norm([p.grad for p in model.parameters() if p.grad is not None], 1.0)
         opt.step()
         sched.step()
-        losses.append(float(loss.detach()))
+        losses.append(float(loss))
         accs.append(float(acc))
         if log_every and (step % log_every == 0 or step == steps - 1):
             print("step %4d loss %.4f acc %.3f" % (step, losses[-1], accs[-1]), flush=True)
