@@ -52,12 +52,18 @@ template <typename T> __device__ __forceinline__ u32x4 all_ninf() {
     const uint32_t u = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
     return u32x4{u, u, u, u};
 }
+// (fmaxf would first quiet every operand, an instruction each; a NaN shows in the sums)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 template <int N>
 __device__ __forceinline__ float max_of(const float (&v)[N]) {
-    float m = fmaxf(v[0], v[1]);
+    float m = max3(v[0], v[1], v[2]);
 #pragma unroll
-    for (int i = 2; i < N; i += 2) m = fmaxf(fmaxf(v[i], v[i + 1]), m);
-    return m;
+    for (int i = 3; i + 1 < N; i += 2) m = max3(m, v[i], v[i + 1]);
+    return max3(m, v[N - 1], v[N - 1]);
 }
 __device__ __forceinline__ float exp_f(float d) { return fast_exp2(d * kLog2e); }
 
@@ -114,34 +120,90 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
     return (uint64_t)hi << 32 | lo;
 }
 
+// Distances from the maximum in units of log 2, l log2(e) - m2, one instruction
+// each: m2 is m log2(e) rounded, off by `off`, which shifts every exponent of the
+// row alike and is taken out of the sums (exp2(l log2(e) - m2) = 2^off exp(l - m)).
+// A row whose maximum is past 2^20 (where `off` could be any size), infinite or
+// NaN is `steep`: it takes l - m itself, element by element from memory.
+struct Scale {
+    float m, m2, off;
+    bool steep;
+    __device__ __forceinline__ explicit Scale(float max) : m(max), m2(max * kLog2e), off(__builtin_fmaf(max, kLog2e, -m2)) {
+        steep = !(fabsf(max) < 1048576.f);
+        if (steep) off = 0.f;
+    }
+    __device__ __forceinline__ float of(float l) const { return __builtin_fmaf(l, kLog2e, -m2); }
+};
+
 // What a row's gradient needs: dl_j = p_j (f + h log p_j) + [j = t] a.
 struct RowGrad {
     float m, ls, f, h, a;
     int64_t t;
     bool zero;
 };
-__device__ __forceinline__ RowGrad row_grad(int64_t r, const LogprobArgs& a, const LogprobGrad& g, float m,
-                                            float ls, float ent) {
+// What a row's results need beside its logits, asked for ahead of them: the
+// target, its logit, the row's weights.
+struct RowIn {
+    int64_t t;
+    float at_t, dlogprob, dentropy, dlse;
+    bool has;
+};
+template <typename T>
+__device__ __forceinline__ RowIn row_in(int64_t r, const LogprobArgs& a, const LogprobGrad* g) {
+    RowIn o{-1, 0.f, 0.f, 0.f, 0.f, false};
+    if (a.targets) {
+        o.t = a.targets[r];
+        o.has = o.t != a.ignore_index;
+        if (a.logprob && o.has && o.t >= 0 && o.t < a.vocab) o.at_t = to_f(((const T*)a.logits)[r * a.stride + o.t]);
+    }
+    if (g) {
+        if (g->dlogprob) o.dlogprob = g->dlogprob[r];
+        if (g->dentropy) o.dentropy = g->dentropy[r];
+        if (g->dlse) o.dlse = g->dlse[r];
+    }
+    return o;
+}
+__device__ __forceinline__ RowGrad row_grad(const RowIn& in, int64_t vocab, float m, float ls, float ent) {
     RowGrad o;
-    o.t = a.targets ? a.targets[r] : a.ignore_index;
-    const bool has = a.targets && o.t != a.ignore_index;
-    o.a = has && g.dlogprob ? g.dlogprob[r] : 0.f;
-    if (has && (o.t < 0 || o.t >= a.vocab)) o.a = __builtin_nanf("");
-    if (!has) o.t = -1;
-    const float dh = g.dentropy ? g.dentropy[r] : 0.f;
-    o.f = (g.dlse ? g.dlse[r] : 0.f) - o.a - (g.dentropy ? dh * ent : 0.f);
-    o.h = -dh;
+    o.t = in.has ? in.t : -1;
+    o.a = in.has ? in.dlogprob : 0.f;
+    if (in.has && (in.t < 0 || in.t >= vocab)) o.a = __builtin_nanf("");
+    o.f = in.dlse - o.a - (in.dentropy != 0.f ? in.dentropy * ent : 0.f);
+    o.h = -in.dentropy;
     const bool none = m == -INFINITY;  // nothing but -infinity
     o.m = none ? 0.f : m;
     o.ls = none ? 0.f : ls;
-    o.zero = o.a == 0.f && o.f == 0.f && dh == 0.f;
+    o.zero = o.a == 0.f && o.f == 0.f && o.h == 0.f;
     return o;
 }
-template <bool ENT>
 __device__ __forceinline__ float grad_of(const RowGrad& g, float l) {
     const float q = (l - g.m) - g.ls, p = exp_f(q);
     // (p is 0 in float long before -200)
-    return p * (ENT ? g.f + g.h * fmaxf(q, -200.f) : g.f);
+    return p * (g.f + g.h * fmaxf(q, -200.f));
+}
+// The same in a Scale's units, e (a + b d) with d its distance and e = exp2(d):
+// with s' the sum of the e, p = e / s' and log p = d log 2 - log s'.
+struct FastGrad {
+    Scale sc;
+    float a, b;
+    __device__ __forceinline__ FastGrad(const RowGrad& g, const Scale& scale, float inv_s, float log_s)
+        : sc(scale), a(inv_s * (g.f - g.h * log_s)), b(inv_s * g.h * kLn2) {}
+    template <bool ENT>
+    __device__ __forceinline__ float of(float l) const {
+        const float d = sc.of(l), e = fast_exp2(d);
+        return ENT ? e * __builtin_fmaf(fmaxf(d, kFar), b, a) : e * a;
+    }
+};
+// The gradients of vector `raw` at element j of the row, with the target's own term.
+template <bool ENT, int N>
+__device__ __forceinline__ void grads_of(const FastGrad& f, const RowGrad& g, int64_t j, float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = f.of<ENT>(v[i]);
+    const int64_t hot = g.t - j;
+    if (hot >= 0 && hot < N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += i == hot ? g.a : 0.f;
+    }
 }
 
 // A vector's elements, stored at any alignment of an element.
@@ -159,10 +221,13 @@ __device__ __forceinline__ void store_any(float* p, const float (&v)[N]) {
     for (int i = 0; i < N; i += 4) *reinterpret_cast<mem*>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
-// A stretch of a row cut at 16-byte boundaries: `nv` whole vectors from element
-// `head`, and head + tail single elements around them (fewer than 16).  A stretch of
-// 2 kVec elements or more has a whole vector.
-template <typename T>
+// A stretch of a row cut at boundaries of ALIGN bytes: `nv` whole vectors from
+// element `head`, and head + tail single elements around them, one per thread.  16
+// bytes for a wave's rows; 128 for a workgroup's, so that its waves' accesses cover
+// whole lines (16384 rows of 50257 bf16, forward and gradient: 733 us, 696 so).  A
+// stretch of 2 ALIGN bytes or more has a whole vector.
+constexpr int align_for(int tpr) { return tpr >= 256 ? 128 : 16; }
+template <typename T, int ALIGN>
 struct Cut {
     const T* p;
     int64_t n;
@@ -174,7 +239,7 @@ struct Cut {
             nv = 0;
             return;
         }
-        const int h = (int)(((16 - ((uintptr_t)q & 15)) & 15) / sizeof(T));
+        const int h = (int)(((ALIGN - (uintptr_t)q % ALIGN) % ALIGN) / sizeof(T));
         head = h < len ? h : (int)len;
         nv = (int)((len - head) / kVec<T>);
         edges = (int)(len - (int64_t)nv * kVec<T>);
@@ -304,8 +369,7 @@ struct Part {
 struct RowStat {
     float m, ls;  // 0 in a row of nothing but -infinity
 };
-template <typename T>
-__device__ __forceinline__ RowStat put_row(const LogprobArgs& a, int64_t r, float m, float s, float c, bool write, float& ent) {
+__device__ __forceinline__ RowStat put_row(const LogprobArgs& a, int64_t r, const RowIn& in, float m, float s, float c, bool write, float& ent) {
     const bool none = s == 0.f;
     const float ls = none ? -INFINITY : logf(s);
     ent = none ? 0.f : ls - c / s;
@@ -314,13 +378,7 @@ __device__ __forceinline__ RowStat put_row(const LogprobArgs& a, int64_t r, floa
         if (a.row_max) a.row_max[r] = none ? -INFINITY : m;
         if (a.log_sum) a.log_sum[r] = ls;
         if (a.entropy) a.entropy[r] = ent;
-        if (a.logprob) {
-            const int64_t t = a.targets[r];
-            float v = 0.f;
-            if (t != a.ignore_index)
-                v = t < 0 || t >= a.vocab ? __builtin_nanf("") : (to_f(((const T*)a.logits)[r * a.stride + t]) - o.m) - o.ls;
-            a.logprob[r] = v;
-        }
+        if (a.logprob) a.logprob[r] = !in.has ? 0.f : in.t < 0 || in.t >= a.vocab ? __builtin_nanf("") : (in.at_t - o.m) - o.ls;
     }
     return o;
 }
@@ -329,8 +387,27 @@ struct SegArgs {
     int nseg;
     int64_t len;    // elements of a segment
     Part* part;     // [rows][nseg]
-    uint64_t* top;  // [rows][nseg][k], largest first; 0 past a segment's elements
+    uint64_t* top;  // [rows][k][nseg], a segment's largest first; 0 past its elements
 };
+
+// The gradients of a steep row's vectors `from`, from + TPR, ... below `to`, and of
+// an edge element.
+template <typename T, typename GT, int TPR>
+__device__ __forceinline__ void put_steep(const Cut<T, align_for(TPR)>& cut, GT* out, const RowGrad& g, int from, int to, bool has_edge) {
+    constexpr int V = kVec<T>;
+    for (int v = from; v < to; v += TPR) {
+        float l[V];
+        unpack(cut.load(v), l);
+        const int64_t j = cut.at(v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) l[i] = grad_of(g, l[i]) + (j + i == g.t ? g.a : 0.f);
+        store_any(out + j, l);
+    }
+    if (has_edge) {
+        const int64_t j = cut.edge(threadIdx.x % TPR);
+        out[j] = from_f<GT>(grad_of(g, to_f(cut.p[j])) + (j == g.t ? g.a : 0.f));
+    }
+}
 
 // Waves a SIMD is to hold (by the registers of NV packed vectors), and with them
 // the workgroups of a CU: the grid of the whole-row kernels.
@@ -347,12 +424,13 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
     const int64_t items = a.rows * (SEG ? sg.nseg : 1), step = (int64_t)gridDim.x * gridDim.y;
     const auto cut_of = [&](int64_t item) {
         const int64_t r = SEG ? item / sg.nseg : item, e0 = SEG ? (item - r * sg.nseg) * sg.len : 0;
-        return Cut<T>((const T*)a.logits + r * a.stride + e0, SEG ? (a.vocab - e0 < sg.len ? a.vocab - e0 : sg.len) : a.vocab, NV == 0);
+        return Cut<T, align_for(TPR)>((const T*)a.logits + r * a.stride + e0, SEG ? (a.vocab - e0 < sg.len ? a.vocab - e0 : sg.len) : a.vocab, NV == 0);
     };
     for (int64_t item = flat_block(); item < items; item += step) {
         const int64_t r = SEG ? item / sg.nseg : item;
         const uint32_t e0 = SEG ? (uint32_t)((item - r * sg.nseg) * sg.len) : 0;
-        const Cut<T> cut = cut_of(item);
+        const auto cut = cut_of(item);
+        const RowIn in = SEG ? RowIn{} : row_in<T>(r, a, GRAD ? &g : nullptr);
         u32x4 raw[NV > 0 ? NV : 1];
         // (past the row its last vector again: no branch keeps the loads apart)
 #pragma unroll
@@ -397,22 +475,36 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
         if constexpr (TOP) {
             if (!by_rounds) top.bound(by);  // (the other waves go on)
         }
+        const Scale scale(m);
         float s = 0.f, c = 0.f;
+        if (!scale.steep) {
 #pragma unroll
-        for (int q = 0; q < NV; ++q) {
-            float v[V];
-            unpack(again(raw[q]), v);
+            for (int q = 0; q < NV; ++q) {
+                float v[V];
+                unpack(again(raw[q]), v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = v[i] - m, e = exp_f(d);
-                s += e;
-                c += e * fmaxf(d, kFar);  // (the maximum drops a NaN, e keeps it)
+                for (int i = 0; i < V; ++i) {
+                    const float d = scale.of(v[i]), e = fast_exp2(d);
+                    s += e;
+                    c += e * fmaxf(d, kFar);  // (the maximum drops a NaN, e keeps it)
+                }
             }
-        }
-        {
-            const float d = edge - m, e = exp_f(d);
+            const float d = scale.of(edge), e = fast_exp2(d);
             s += e;
             c += e * fmaxf(d, kFar);
+        } else {
+            const auto add = [&](float l) {
+                const float d = l - m, e = exp_f(d);
+                s += e;
+                c += e * fmaxf(d * kLog2e, kFar);
+            };
+            for (int v = tid; v < cut.nv; v += TPR) {
+                float l[V];
+                unpack(cut.load(v), l);
+#pragma unroll
+                for (int i = 0; i < V; ++i) add(l[i]);
+            }
+            if (has_edge) add(edge);
         }
         s = wave_sum(s);
         c = wave_sum(c);
@@ -429,19 +521,25 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
                 c += sh.st.c[w];
             }
         }
+        const float scaled_sum = s;
+        {
+            const float unit = fast_exp2(-scale.off);
+            c = (c - s * scale.off) * (unit * kLn2);
+            s *= unit;
+        }
         float ent = 0.f;
         RowStat row{m, 0.f};
         if constexpr (SEG) {
             if (tid == 0) sg.part[item] = Part{m, s, c, 0.f};
         } else {
-            row = put_row<T>(a, r, m, s, c, tid == 0, ent);
+            row = put_row(a, r, in, m, s, c, tid == 0, ent);
         }
 
         if constexpr (TOP) {
             const bool orderly = s == s;  // a NaN has no place among the floats compared
             const auto emit = [&](int at, uint64_t key) {
                 if constexpr (SEG) {
-                    if (at < cut.n) sg.top[item * a.top_k + at] = key;
+                    if (at < cut.n) sg.top[(r * a.top_k + at) * sg.nseg + (item - r * sg.nseg)] = key;
                 } else {
                     a.top_ids[r * a.top_k + at] = key_index(key);
                     a.top_logprobs[r * a.top_k + at] = (key_value(key) - row.m) - row.ls;
@@ -516,29 +614,29 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
                 }
                 __syncthreads();
                 if constexpr (SEG) {
-                    if (tid >= cut.n && tid < a.top_k) sg.top[item * a.top_k + tid] = 0;
+                    if (tid >= cut.n && tid < a.top_k) sg.top[(r * a.top_k + tid) * sg.nseg + (item - r * sg.nseg)] = 0;
                 }
                 top.finish(by, orderly, emit, each);
             }
         }
 
         if constexpr (GRAD) {
-            const RowGrad rg = row_grad(r, a, g, s == 0.f ? -INFINITY : m, row.ls, ent);
+            const RowGrad rg = row_grad(in, a.vocab, s == 0.f ? -INFINITY : m, row.ls, ent);
             GT* out = (GT*)g.dlogits + r * g.stride;
+            const FastGrad fast(rg, scale, 1.0f / scaled_sum, row.ls + scale.off * kLn2);
             const auto put = [&](auto with_entropy) {
                 constexpr bool ENT = decltype(with_entropy)::value;
 #pragma unroll
                 for (int q = 0; q < NV; ++q) {
                     float v[V];
                     unpack(again(raw[q]), v);
-                    const int hot = (int)(rg.t - cut.head) - (tid + q * TPR) * V;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) v[i] = grad_of<ENT>(rg, v[i]) + (i == hot ? rg.a : 0.f);
-                    if (tid + q * TPR < cut.nv) store_any(out + cut.at(tid + q * TPR), v);
+                    const int64_t j = cut.at(tid + q * TPR);
+                    grads_of<ENT>(fast, rg, j, v);
+                    if (tid + q * TPR < cut.nv) store_any(out + j, v);
                 }
                 if (has_edge) {
                     const int64_t j = cut.edge(tid);
-                    out[j] = from_f<GT>(grad_of<ENT>(rg, edge) + (j == rg.t ? rg.a : 0.f));
+                    out[j] = from_f<GT>(fast.of<ENT>(edge) + (j == rg.t ? rg.a : 0.f));
                 }
             };
             if (rg.zero) {
@@ -548,6 +646,8 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
                     if (tid + q * TPR < cut.nv) store_any(out + cut.at(tid + q * TPR), z);
                 }
                 if (has_edge) out[cut.edge(tid)] = from_f<GT>(0.f);
+            } else if (scale.steep) {
+                put_steep<T, GT, TPR>(cut, out, rg, tid, cut.nv, has_edge);
             } else if (rg.h != 0.f) {
                 put(std::true_type{});
             } else {
@@ -565,11 +665,20 @@ __global__ __launch_bounds__(256) void k_token_logprobs_join(const LogprobArgs a
     if (r >= a.rows) return;
     const int tid = threadIdx.x, wave = tid >> 6;
     const Part* part = sg.part + r * sg.nseg;
+    const RowIn in = row_in<T>(r, a, nullptr);
+    // candidates in the order of their places, so that the segments' first ones spread
+    // over the lanes; a thread keeps its first four
     const int n = sg.nseg * a.top_k;
+    const uint64_t* cand = sg.top + r * n;
+    uint64_t kept[4] = {};
+    if constexpr (TOP) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kept[i] = tid + 256 * i < n ? cand[tid + 256 * i] : 0;
+    }
     const auto each = [&](auto f) {
-        // candidate i: place i / nseg of segment i % nseg, so that the first places
-        // spread over the lanes
-        for (int i = tid; i < n; i += 256) f(sg.top[(r * sg.nseg + i % sg.nseg) * a.top_k + i / sg.nseg]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f(kept[i]);
+        for (int i = tid + 1024; i < n; i += 256) f(cand[i]);
     };
     Top<256, TOP> top(sh, a.top_k);
     if constexpr (TOP) {
@@ -601,7 +710,7 @@ __global__ __launch_bounds__(256) void k_token_logprobs_join(const LogprobArgs a
     s = sh.st.s[0] + sh.st.s[1] + sh.st.s[2] + sh.st.s[3];
     c = sh.st.c[0] + sh.st.c[1] + sh.st.c[2] + sh.st.c[3];
     float ent;
-    const RowStat row = put_row<T>(a, r, m, s, c, tid == 0, ent);
+    const RowStat row = put_row(a, r, in, m, s, c, tid == 0, ent);
     if constexpr (TOP) {
         const uint64_t bound = sh.top.bound;
         if (top.mine >= bound) each([&](uint64_t key) { if (key >= bound) top.push(key); });
@@ -624,9 +733,9 @@ __global__ __launch_bounds__(256) void k_token_logprobs_bwd(const LogprobArgs a,
     for (; item < items; item += step) {
         const int64_t r = item / stretches;
         const int v0 = (int)(item - r * stretches) * (TPR * NV);
-        const Cut<T> cut((const T*)a.logits + r * a.stride, a.vocab);
+        const Cut<T, align_for(TPR)> cut((const T*)a.logits + r * a.stride, a.vocab);
         GT* out = (GT*)g.dlogits + r * g.stride;
-        const RowGrad rg = row_grad(r, a, g, a.row_max[r], a.log_sum[r], g.dentropy ? a.entropy[r] : 0.f);
+        const RowGrad rg = row_grad(row_in<T>(r, a, &g), a.vocab, a.row_max[r], a.log_sum[r], g.dentropy ? a.entropy[r] : 0.f);
         const bool has_edge = v0 == 0 && tid < cut.edges;
         if (rg.zero) {
             const float z[V] = {};
@@ -638,6 +747,11 @@ __global__ __launch_bounds__(256) void k_token_logprobs_bwd(const LogprobArgs a,
             if (has_edge) out[cut.edge(tid)] = from_f<GT>(0.f);
             continue;
         }
+        const Scale scale(rg.m);
+        if (scale.steep) {
+            put_steep<T, GT, TPR>(cut, out, rg, v0 + tid, v0 + TPR * NV < cut.nv ? v0 + TPR * NV : cut.nv, has_edge);
+            continue;
+        }
         u32x4 raw[NV];
 #pragma unroll
         for (int q = 0; q < NV; ++q) {
@@ -645,6 +759,9 @@ __global__ __launch_bounds__(256) void k_token_logprobs_bwd(const LogprobArgs a,
             if (v < cut.nv) raw[q] = cut.load(v);
         }
         const float edge = has_edge ? to_f(cut.p[cut.edge(tid)]) : 0.f;
+        // exp(-log s') with the product's rounding carried along: it would be the largest
+        const float log_s = rg.ls + scale.off * kLn2, hi = rg.ls * kLog2e, lo = __builtin_fmaf(rg.ls, kLog2e, -hi) + scale.off;
+        const FastGrad fast(rg, scale, fast_exp2(-hi) * fast_exp2(-lo), log_s);
         const auto put = [&](auto with_entropy) {
             constexpr bool ENT = decltype(with_entropy)::value;
 #pragma unroll
@@ -653,15 +770,14 @@ __global__ __launch_bounds__(256) void k_token_logprobs_bwd(const LogprobArgs a,
                 if (v < cut.nv) {
                     float l[V];
                     unpack(raw[q], l);
-                    const int64_t j = cut.at(v), hot = rg.t - j;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) l[i] = grad_of<ENT>(rg, l[i]) + (i == hot ? rg.a : 0.f);
+                    const int64_t j = cut.at(v);
+                    grads_of<ENT>(fast, rg, j, l);
                     store_any(out + j, l);
                 }
             }
             if (has_edge) {
                 const int64_t j = cut.edge(tid);
-                out[j] = from_f<GT>(grad_of<ENT>(rg, edge) + (j == rg.t ? rg.a : 0.f));
+                out[j] = from_f<GT>(fast.of<ENT>(edge) + (j == rg.t ? rg.a : 0.f));
             }
         };
         if (rg.h != 0.f) put(std::true_type{});

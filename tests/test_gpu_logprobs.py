@@ -104,7 +104,9 @@ def check_grad(ref, t, dlp, dent, dlse, got, gdtype):
     ref_g = p * (z - a - h * (qs + H))
     for r in np.flatnonzero(has):
         ref_g[r, t.reshape(-1)[r]] += a[r, 0]
-    scale = np.abs(a) + np.abs(z) + np.abs(h) * (np.abs(qs) + H + ref["mean_d"][:, None])
+    # log p = d - log_sum inherits log_sum's K u as it is, however small log p: a row of one token has log p = entropy = 0,
+    # and dentropy (log p + entropy) there is dentropy times those K u, not times 0
+    scale = np.abs(a) + np.abs(z) + np.abs(h) * (1 + np.abs(qs) + H + ref["mean_d"][:, None])
     rel = 2 * K * U + 8 * U * np.abs(qs)
     bound = STEP[gdtype] * np.abs(ref_g) + p * scale * rel + U * np.abs(a) * (np.abs(ref_g) > 0) * 4 + 1e-37
     close(got.reshape(R, V), ref_g, bound, "dlogits")
@@ -387,3 +389,25 @@ def test_other_stream_and_refusals():
         dart.token_logprobs(l.half(), t)
     with pytest.raises(dart.DartError):
         dart.token_logprobs_grad(l.float(), t, ref["logprob"], grad_dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("V,R", [(40, 1), (700, 1), (9000, 1), (50257, 1), (9000, 600)])
+def test_large_common_parts(V, R):
+    """Maxima on both sides of 2^20, where the exponents' common rounding is taken out or the distances are formed."""
+    print("\n[gpu-case] logprobs large common parts V=%d x%d" % (V, R), flush=True)
+    rng = np.random.default_rng(V)
+    at = [2.0 ** 19.9, 2.0 ** 20, 2.0 ** 20.1, -2.0 ** 19.9, -2.0 ** 20.5, 3e4, -3e5, 1e9, 1e30, -2e38, 3e38, 77.0]
+    spread = [1.0, 1.0, 2.0, 0.5, 1.0, 3.0, 3.0, 100.0, 1e24, 1e32, 1e32, 0.0]
+    a = np.tile(np.stack([m + w * rng.standard_normal(V) for m, w in zip(at, spread)]), (-(-R // len(at)), 1))
+    for dtype in ("fp32", "bf16"):
+        l = tensor(a, dtype)
+        t = rng.integers(0, V, len(a))
+        k = min(V, 9)
+        r = dart.token_logprobs(l, ids(t), top_k=k)
+        ref = check_forward(l, t, r, k)
+        dlp, dent = tensor(rng.standard_normal(len(a))), tensor(rng.standard_normal(len(a)))
+        g = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], targets=ids(t), dlogprob=dlp, entropy=r["entropy"], dentropy=dent)
+        check_grad(ref, t, dlp, dent, None, g, dtype)
+        one = dart.token_logprobs_grad(l.clone(), ids(t), dlp, dentropy=dent, top_k=k)
+        check_forward(l, t, one, k)
+        check_grad(ref, t, dlp, dent, None, one["dlogits"], dtype)
