@@ -395,7 +395,7 @@ dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t
  * probability 0.  A row of nothing else has row_max = log_sum = -infinity,
  * entropy 0 and, for every token, logprob -infinity.  A logit of NaN or
  * +infinity makes the row's log_sum, logprob and entropy NaN.
- *   logits   [rows][row_stride] storage dtype, any alignment
+ *   logits   [rows][row_stride] storage dtype, any alignment; vocab <= 2^24
  *   targets  [rows] int64, or NULL (then logprob is NULL)
  *   logprob, entropy, row_max, log_sum [rows] float, each may be NULL
  *   top_ids [rows][top_k] int64, top_logprobs [rows][top_k] float; 0 <= top_k

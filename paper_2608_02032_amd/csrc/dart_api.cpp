@@ -507,7 +507,7 @@ dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t
 static dart_status check_logits(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
                                 int32_t grad_dtype, int32_t top_k) {
     if (rows < 0 || vocab < 1) return fail(DART_ERR_INVALID_ARG, "rows must be >= 0 and vocab >= 1");
-    if (vocab > 2147483647LL) return fail(DART_ERR_UNSUPPORTED, "vocab must be < 2^31");
+    if (vocab > (1 << 24)) return fail(DART_ERR_UNSUPPORTED, "vocab %lld not supported (at most 2^24)", (long long)vocab);
     if (row_stride < vocab)
         return fail(DART_ERR_INVALID_ARG, "row_stride (%lld) < vocab (%lld)", (long long)row_stride, (long long)vocab);
     if (too_large(rows, row_stride)) return fail(DART_ERR_UNSUPPORTED, "too many rows");

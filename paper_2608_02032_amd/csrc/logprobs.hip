@@ -812,7 +812,8 @@ Plan plan_for(int64_t rows, int64_t vocab, int dtype, int top_k, bool grad) {
     int64_t want = (device_cu_count() + rows - 1) / rows;
     int nv = 8;
     while (nv > 2 && (vocab + 256 * nv * vec - 1) / (256 * nv * vec) < want) nv /= 2;
-    // (a segment takes up to `most` elements; even ones leave no short last one)
+    // (even segments: the last one is shorter than the others by less than their
+    // number, below 2^24 / 8192, and so never too short for a whole vector)
     const int64_t each = (int64_t)256 * nv * vec, nseg = (vocab + each - 1) / each;
     return {(int)nseg, 256, nv, (vocab + nseg - 1) / nseg};
 }

@@ -411,3 +411,18 @@ def test_large_common_parts(V, R):
         one = dart.token_logprobs_grad(l.clone(), ids(t), dlp, dentropy=dent, top_k=k)
         check_forward(l, t, one, k)
         check_grad(ref, t, dlp, dent, None, one["dlogits"], dtype)
+
+
+@pytest.mark.parametrize("dtype,V", [("fp32", (1 << 24) - 4095), ("bf16", 1 << 24), ("bf16", 4096 * 255 + 1), ("fp32", 2048 * 200 + 3)])
+def test_many_segments(dtype, V):
+    """Up to 2048 segments of a row, and segments that come out uneven."""
+    import torch
+    print("\n[gpu-case] logprobs many segments %s V=%d" % (dtype, V), flush=True)
+    rng = np.random.default_rng(V)
+    l = tensor(rng.standard_normal((1, V), dtype=np.float32) * 2, dtype)
+    t = np.array([V - 1])
+    r = dart.token_logprobs(l, ids(t), top_k=32)
+    check_forward(l, t, r, 32)
+    one = dart.token_logprobs_grad(l, ids(t), torch.ones(1, device="cuda"), top_k=1)
+    assert int(one["top_ids"][0, 0]) == int(r["top_ids"][0, 0])
+    assert abs(float(one["dlogits"].double().sum())) <= (2.0 ** -8 if dtype == "bf16" else 1e-4)   # sums to 0; half steps, about V of them of 1 / V

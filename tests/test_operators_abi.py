@@ -64,7 +64,8 @@ def lp(lib, rows=4, vocab=100, stride=104, dtype=BF16, logits=P, targets=2 * P, 
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(rows=-1), INVALID), (dict(vocab=0), INVALID), (dict(vocab=1 << 31, stride=1 << 31), UNSUPPORTED), (dict(stride=99), INVALID),
+    (dict(rows=-1), INVALID), (dict(vocab=0), INVALID), (dict(vocab=1 << 31, stride=1 << 31), UNSUPPORTED),
+    (dict(vocab=(1 << 24) + 1, stride=1 << 25), UNSUPPORTED), (dict(stride=99), INVALID),
     (dict(dtype=-1), INVALID), (dict(k=-1), INVALID), (dict(k=101), INVALID), (dict(k=33), UNSUPPORTED), (dict(vocab=2, k=3), INVALID),
     (dict(logits=None), INVALID), (dict(targets=None), INVALID), (dict(ids=None), INVALID), (dict(tops=None), INVALID),
     (dict(rows=1 << 60), UNSUPPORTED)])
