@@ -16,6 +16,8 @@
 // row's sums, and a lane keeps its columns' weights for all its rows.  In the
 // backward it keeps their sums of dw and db too: one partial row per
 // workgroup, added in a second launch in a fixed order.
+// 16384 rows of 4096 bf16 with residual: forward 80 us, 6.7 TB/s, backward 91 us,
+// 5.9 TB/s, and 4 us to add the partial rows; 32768 rows of 768: 35 and 38 us.
 #include "dart_common.hpp"
 #include "dart_internal.hpp"
 
@@ -253,20 +255,26 @@ __global__ __launch_bounds__(block_threads(TPR)) void k_layernorm_bwd(const Norm
     constexpr int GR = block_threads(TPR) / TPR;
     constexpr int W = TPR * ITEMS * V;  // columns, with those past the row
     __shared__ float s_sum[3][2][TPR > 64 ? TPR / 64 : 1];
-    __shared__ float s_col[GR > 1 ? (GR - 1) * W : 1];
+    constexpr bool keep = keeps_weights(TPR, ITEMS * V), ahead = keep;
+    // the column sums of the groups but the first; of rows whose weights are not
+    // kept all of them, from the start
+    __shared__ float s_col[!keep ? 2 * W : GR > 1 ? (GR - 1) * W : 1];
     const int lane = threadIdx.x % TPR, group = row_group<TPR>();
     const T* x = (const T*)a.x;
     const GT* dout = (const GT*)a.dout;
     const GT* dsum = (const GT*)a.dsum;
     RowSum<3, TPR> row_sum{s_sum, 0};
-    constexpr bool keep = keeps_weights(TPR, ITEMS * V), ahead = keep;
-    float wv[keep ? ITEMS : 1][V], aw[ITEMS][V], ab[ITEMS][V];
+    float wv[keep ? ITEMS : 1][V], aw[keep ? ITEMS : 1][V], ab[keep ? ITEMS : 1][V];
+    const auto slot = [&](int q, int i) { return (i * ITEMS + q) * TPR + lane; };
     const Columns<V, TPR, ITEMS, RAGGED> cols(lane, a.D);
 #pragma unroll
     for (int q = 0; q < ITEMS; ++q) {
         if constexpr (keep) load_cols(a.w, cols.first[q], 1.f, wv[q]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) aw[q][i] = ab[q][i] = 0.f;
+        for (int i = 0; i < V; ++i) {
+            if constexpr (keep) aw[q][i] = ab[q][i] = 0.f;
+            else s_col[slot(q, i)] = s_col[W + slot(q, i)] = 0.f;
+        }
     }
     RawT<T, V> xr[ITEMS] = {};
     RawT<GT, V> dr[ITEMS] = {}, sr[ITEMS] = {};
@@ -334,8 +342,13 @@ __global__ __launch_bounds__(block_threads(TPR)) void k_layernorm_bwd(const Norm
                 for (int i = 0; i < V; ++i) {
                     const float xh = v[q][i] * inv;
                     o[i] = inv * (d[i] * wv[keep ? q : 0][i] - m1 - xh * m2) + (dsum ? e[i] : 0.f);
-                    aw[q][i] += d[i] * xh;
-                    ab[q][i] += d[i];
+                    if constexpr (keep) {
+                        aw[q][i] += d[i] * xh;
+                        ab[q][i] += d[i];
+                    } else {
+                        s_col[slot(q, i)] += d[i] * xh;
+                        s_col[W + slot(q, i)] += d[i];
+                    }
                 }
                 if (cols.any(q)) store_v((GT*)a.dx + r * a.D + cols.first[q], o);
             }
@@ -343,41 +356,58 @@ __global__ __launch_bounds__(block_threads(TPR)) void k_layernorm_bwd(const Norm
     }
     // the groups' column sums in the order of the groups
     float* part = a.part + (int64_t)blockIdx.x * 2 * a.D;
-    const auto finish = [&](float (&acc)[ITEMS][V], float* out) {
-        if constexpr (GR > 1) {
-            __syncthreads();
-            if (group > 0) {
+    const auto put = [&](int q, const float (&v)[V], float* out) {
+        const int c = cols.first[q];
+        if constexpr (RAGGED || V == 1) {
 #pragma unroll
-                for (int q = 0; q < ITEMS; ++q)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) s_col[(group - 1) * W + (i * ITEMS + q) * TPR + lane] = acc[q][i];
+            for (int i = 0; i < V; ++i) {
+                if (cols.own(q, i)) out[c + i] = v[i];
             }
-            __syncthreads();
-        }
-        if (group > 0) return;
+        } else if (cols.any(q)) {
 #pragma unroll
-        for (int q = 0; q < ITEMS; ++q) {
-            for (int k = 0; k + 1 < GR; ++k) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) acc[q][i] += s_col[k * W + (i * ITEMS + q) * TPR + lane];
-            }
-            const int c = cols.first[q];
-            if constexpr (RAGGED || V == 1) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    if (cols.own(q, i)) out[c + i] = acc[q][i];
-                }
-            } else if (cols.any(q)) {
-#pragma unroll
-                for (int i = 0; i < V; i += 4) {
-                    const float o[4] = {acc[q][i], acc[q][i + 1], acc[q][i + 2], acc[q][i + 3]};
-                    store4(out + c + i, o);
-                }
+            for (int i = 0; i < V; i += 4) {
+                const float o[4] = {v[i], v[i + 1], v[i + 2], v[i + 3]};
+                store4(out + c + i, o);
             }
         }
     };
-    finish(aw, part);
-    finish(ab, part + a.D);
+    if constexpr (!keep) {
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            float w[V], b[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                w[i] = s_col[slot(q, i)];
+                b[i] = s_col[W + slot(q, i)];
+            }
+            put(q, w, part);
+            put(q, b, part + a.D);
+        }
+    } else {
+        const auto finish = [&](float (&acc)[ITEMS][V], float* out) {
+            if constexpr (GR > 1) {
+                __syncthreads();
+                if (group > 0) {
+#pragma unroll
+                    for (int q = 0; q < ITEMS; ++q)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) s_col[(group - 1) * W + slot(q, i)] = acc[q][i];
+                }
+                __syncthreads();
+            }
+            if (group > 0) return;
+#pragma unroll
+            for (int q = 0; q < ITEMS; ++q) {
+                for (int k = 0; k + 1 < GR; ++k) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[q][i] += s_col[k * W + slot(q, i)];
+                }
+                put(q, acc[q], out);
+            }
+        };
+        finish(aw, part);
+        finish(ab, part + a.D);
+    }
 }
 
 // Waves a CU holds of a form that keeps E elements per lane (by its registers): the
@@ -401,10 +431,10 @@ int64_t bwd_cap() { return (int64_t)device_cu_count() * 4; }
 
 // The form that holds a row of n vectors: few idle lanes, few lanes to exchange
 // sums between, and at most 16 elements per lane (beyond that too few waves are
-// resident).  Rows of more than 8192 spill registers in the backward, of 16384
-// bf16 at 2.2 TB/s against 5.4 of 4096.  Rows that are no multiple of a vector, at
-// any alignment: 16384 rows of 4095 bf16 forward 5.0 TB/s, of 4096 6.7 (element by
-// element 1.5).
+// resident).  Backward of more than 8192 columns, 16 elements in each of 1024
+// lanes: the column sums stand in LDS (4096 rows of 16384 bf16 136 us, 4.0 TB/s; in
+// registers, spilt, 246).  Rows that are no multiple of a vector, at any alignment:
+// 16384 rows of 4095 bf16 forward 5.0 TB/s, of 4096 6.7 (element by element 1.5).
 #define DART_NORM_FORMS(V, F)                                        \
     if constexpr (V == 8) {                                          \
         if (n <= 16) F(8, 16, 1);                                    \
