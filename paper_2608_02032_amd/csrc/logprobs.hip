@@ -9,13 +9,17 @@
 // A logit of -infinity has p = 0 and takes no part; a row of nothing else has
 // no distribution (m = log s = -infinity, entropy 0, p = 0).
 //
-// Bound by HBM: about ten operations per logit forward and twelve backward, one
-// of them an exponential (a quarter of the rate), against two or four bytes.  A
-// workgroup holds a row, packed as stored, in its registers (up to 131072 bf16
-// or 65536 float): every load of the row is in flight at once, the maximum comes
-// before the exponentials, and the alternatives and the gradient are formed
-// from the registers.  Longer rows, and few rows for the card, are cut into
-// segments, one per workgroup, whose results a second launch joins.
+// Bound by HBM, with the vector units close behind: some eight instructions per
+// logit forward and seven for the gradient, one of each an exponential, against
+// two or four bytes.  A workgroup holds a row, packed as stored, in its registers
+// (up to 131072 bf16 or 65536 float): every load of the row is in flight at once,
+// the maximum comes before the exponentials, and the alternatives and the
+// gradient are formed from the registers.  Longer rows, and few rows for the card,
+// are cut into segments, one per workgroup, whose results a second launch joins.
+// 16384 rows of 50257 bf16: forward and gradient in one call 690 us (4.8 TB/s), the
+// gradient alone 550 us (6.0 TB/s); 8192 rows forward 185 us (4.4 TB/s), with five
+// alternatives 215 us; 4096 rows of 131072 forward 180 us (6.0 TB/s); one row of
+// 131072 with twenty alternatives 13 us in two launches.
 #include "dart_common.hpp"
 #include "dart_internal.hpp"
 
@@ -25,7 +29,7 @@ namespace dart {
 namespace {
 
 constexpr float kLowest = -3.402823466e+38f;
-constexpr float kFar = -1e30f;  // stands for a logit's distance of -infinity where exp is 0
+constexpr float kFar = -200.f;  // stands for any distance below it, where exp and exp2 are 0 in float
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> constexpr int kVec = 16 / sizeof(T);  // elements of 16 bytes
@@ -178,8 +182,7 @@ __device__ __forceinline__ RowGrad row_grad(const RowIn& in, int64_t vocab, floa
 }
 __device__ __forceinline__ float grad_of(const RowGrad& g, float l) {
     const float q = (l - g.m) - g.ls, p = exp_f(q);
-    // (p is 0 in float long before -200)
-    return p * (g.f + g.h * fmaxf(q, -200.f));
+    return p * (g.f + g.h * fmaxf(q, kFar));
 }
 // The same in a Scale's units, e (a + b d) with d its distance and e = exp2(d):
 // with s' the sum of the e, p = e / s' and log p = d log 2 - log s'.

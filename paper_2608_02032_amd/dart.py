@@ -697,13 +697,15 @@ def _logits_args(logits, targets, *others):
 
 def _dlogits(dlogits, logits, grad_dtype, stride, empty):
     """The gradient's tensor: rows at the stride of the logits', so that their
-    alignment is the logits' too."""
+    alignment is the logits' too (dense ones for a slice of much wider rows)."""
     if dlogits is not None:
         if dlogits.shape != logits.shape:
             raise ValueError("dlogits must have the shape of logits")
         return dlogits, _row_stride(dlogits, "dlogits")
     dtype = logits.dtype if grad_dtype is None else grad_dtype
     V = logits.shape[-1]
+    if stride > V + 256:
+        stride = V
     buf = empty(tuple(logits.shape[:-1]) + (stride,), dtype=dtype, device=logits.device)
     return (buf if stride == V else buf[..., :V]), stride
 

@@ -426,3 +426,35 @@ def test_many_segments(dtype, V):
     one = dart.token_logprobs_grad(l, ids(t), torch.ones(1, device="cuda"), top_k=1)
     assert int(one["top_ids"][0, 0]) == int(r["top_ids"][0, 0])
     assert abs(float(one["dlogits"].double().sum())) <= (2.0 ** -8 if dtype == "bf16" else 1e-4)   # sums to 0; half steps, about V of them of 1 / V
+
+
+def test_gradient_of_a_slice_of_wide_rows_is_dense():
+    import torch
+    rng = np.random.default_rng(6)
+    wide = tensor(rng.standard_normal((6, 5000)), "bf16")
+    l, t = wide[:, 100:300], rng.integers(0, 200, 6)
+    one = dart.token_logprobs_grad(l, ids(t), torch.ones(6, device="cuda"))
+    assert one["dlogits"].is_contiguous()
+    check_grad(reference(f64(l), t, 0), t, torch.ones(6, device="cuda"), None, None, one["dlogits"], "bf16")
+    padded = dart.token_logprobs_grad(wide[:, :4990], ids(t), torch.ones(6, device="cuda"))["dlogits"]
+    assert padded.stride(0) == 5000
+
+
+@pytest.mark.parametrize("V,R", [(100, 3), (5000, 2), (60000, 200)])
+def test_masked_logits_stay_without_gradient(V, R):
+    """Whatever the weights: no infinity meets the zero probability of a masked logit."""
+    import torch
+    rng = np.random.default_rng(V)
+    a = rng.standard_normal((R, V))
+    a[:, ::3] = -np.inf
+    a[0] = -np.inf
+    l, t = tensor(a), ids(np.ones(R))
+    big = torch.full((R,), 1e30, device="cuda")
+    r = dart.token_logprobs(l, t)
+    two = dart.token_logprobs_bwd(l, r["row_max"], r["log_sum"], targets=t, dlogprob=big, entropy=r["entropy"], dentropy=big)
+    one = dart.token_logprobs_grad(l, t, big, dentropy=big)["dlogits"]
+    for g in (two, one):
+        assert bool(torch.isfinite(g).all())
+        masked = torch.isneginf(l)
+        masked[0, 1] = False   # the first row's target keeps its own term
+        assert not bool(g[masked].any())
