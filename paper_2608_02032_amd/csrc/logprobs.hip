@@ -16,10 +16,10 @@
 // the maximum comes before the exponentials, and the alternatives and the
 // gradient are formed from the registers.  Longer rows, and few rows for the card,
 // are cut into segments, one per workgroup, whose results a second launch joins.
-// 16384 rows of 50257 bf16: forward and gradient in one call 690 us (4.8 TB/s), the
-// gradient alone 550 us (6.0 TB/s); 8192 rows forward 185 us (4.4 TB/s), with five
-// alternatives 215 us; 4096 rows of 131072 forward 180 us (6.0 TB/s); one row of
-// 131072 with twenty alternatives 13 us in two launches.
+// 16384 rows of 50257 bf16: forward 309 us (5.3 TB/s), the gradient after it 556 us
+// (5.9 TB/s), both in one pass 703 us (4.7 TB/s, what a copy reaches); 8192 rows 157 us,
+// with five alternatives 213; 4096 rows of 131072 forward 179 us (6.0
+// TB/s); one row of 131072 with twenty alternatives 10 us and 8 us for the join.
 #include "dart_common.hpp"
 #include "dart_internal.hpp"
 
@@ -197,7 +197,7 @@ struct FastGrad {
         return ENT ? e * __builtin_fmaf(fmaxf(d, kFar), b, a) : e * a;
     }
 };
-// The gradients of vector `raw` at element j of the row, with the target's own term.
+// The gradients of a vector at element j of the row, with the target's own term.
 template <bool ENT, int N>
 __device__ __forceinline__ void grads_of(const FastGrad& f, const RowGrad& g, int64_t j, float (&v)[N]) {
 #pragma unroll
@@ -800,7 +800,7 @@ Plan plan_for(int64_t rows, int64_t vocab, int dtype, int top_k, bool grad) {
     const int64_t most = 1024 * 16 * vec;
     // long rows without alternatives or gradient in segments of 256 threads, if those
     // are nearly full: more of them are resident, and nothing waits for a whole row
-    // (4096 rows of 131072 bf16 194 us, 5.5 TB/s, whole 242; of 50257 float 136 and 160;
+    // (4096 rows of 131072 bf16 179 us, 6.0 TB/s, whole 242; of 50257 float 134 and 160;
     // but 8192 of 50257 bf16, 0.77 full, 241 and 190, and with five alternatives,
     // which every segment sorts, 4096 of 131072 322 and 286)
     const int64_t full = 256 * 8 * vec, parts = (vocab + full - 1) / full;
@@ -811,7 +811,7 @@ Plan plan_for(int64_t rows, int64_t vocab, int dtype, int top_k, bool grad) {
         for (const auto& f : forms)
             if (f[1] ? vocab <= (int64_t)f[0] * f[1] * vec : vocab < 2 * vec) return {1, f[0], f[1], vocab};
     }
-    // segments for a workgroup per CU, of at least one vector per thread and at most eight
+    // segments for a workgroup per CU, of two to eight vectors per thread
     int64_t want = (device_cu_count() + rows - 1) / rows;
     int nv = 8;
     while (nv > 2 && (vocab + 256 * nv * vec - 1) / (256 * nv * vec) < want) nv /= 2;

@@ -20,6 +20,7 @@ import math
 
 import torch
 import torch.nn as nn
+from torch.autograd.function import once_differentiable
 
 from . import dart
 
@@ -118,6 +119,7 @@ class _Norm(torch.autograd.Function):
         return dart.layernorm(u, w, center=False)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         u, w = ctx.saved_tensors
         g = dart.layernorm_bwd(u, dout.contiguous(), w, center=False)
@@ -136,6 +138,7 @@ class _AddNorm(torch.autograd.Function):
         return s, out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, ds, dout):
         s, w = ctx.saved_tensors
         if dout is None:
@@ -157,6 +160,7 @@ class _TokenLogprobs(torch.autograd.Function):
         return r["logprob"], r["entropy"]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dlogprob, dentropy):
         logits, targets, row_max, log_sum, entropy = ctx.saved_tensors
         dl = dart.token_logprobs_bwd(

@@ -196,3 +196,15 @@ def test_train_mqar_steps():
     from paper_2608_02032_amd import layer, mqar
     losses, accs = layer.train_mqar(3, L=64, R=4, batch=4, vocab=mqar.MqarVocab(16, 16))
     assert len(losses) == len(accs) == 3 and np.all(np.isfinite(losses)) and all(0 <= a <= 1 for a in accs)
+
+
+def test_a_second_derivative_is_refused():
+    import torch
+    from paper_2608_02032_amd import layer
+    u = torch.randn(4, 32, device="cuda", requires_grad=True)
+    w = torch.ones(32, device="cuda", requires_grad=True)
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    for f in (lambda: layer._Norm.apply(u, w), lambda: layer.add_norm(u, u, w)[1], lambda: layer.token_logprobs(u, t)[0]):
+        g, = torch.autograd.grad(f().square().sum(), u, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.sum().backward()
