@@ -16,10 +16,10 @@
 // the maximum comes before the exponentials, and the alternatives and the
 // gradient are formed from the registers.  Longer rows, and few rows for the card,
 // are cut into segments, one per workgroup, whose results a second launch joins.
-// 16384 rows of 50257 bf16: forward 309 us (5.3 TB/s), the gradient after it 556 us
-// (5.9 TB/s), both in one pass 703 us (4.7 TB/s, what a copy reaches); 8192 rows 157 us,
-// with five alternatives 213; 4096 rows of 131072 forward 179 us (6.0
-// TB/s); one row of 131072 with twenty alternatives 10 us and 8 us for the join.
+// 16384 rows of 50257 bf16: forward 287 us (5.7 TB/s), the gradient after it 556 us
+// (5.9 TB/s), both in one pass 680 us (4.8 TB/s, as a copy); with five alternatives
+// 8192 rows take 213 us instead of 147; 4096 rows of 131072 forward 180 us (6.0 TB/s);
+// one row of 131072 with twenty alternatives 10 us and 8 us for the join.
 #include "dart_common.hpp"
 #include "dart_internal.hpp"
 
@@ -103,10 +103,9 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t v, int lane) {
     const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
     return (uint64_t)hi << 32 | lo;
 }
-template <bool LARGEST>
-__device__ __forceinline__ uint32_t wave_pick_u32(uint32_t v) {
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
     const auto dpp = [](auto ctrl, uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(ctrl)::value, 0xF, 0xF, false); };
-    const auto pick = [](uint32_t x, uint32_t y) { return (x < y) == LARGEST ? y : x; };
+    const auto pick = [](uint32_t x, uint32_t y) { return x < y ? y : x; };
     v = pick(v, dpp(std::integral_constant<int, 0xB1>{}, v));
     v = pick(v, dpp(std::integral_constant<int, 0x4E>{}, v));
     v = pick(v, dpp(std::integral_constant<int, 0x141>{}, v));
@@ -117,10 +116,9 @@ __device__ __forceinline__ uint32_t wave_pick_u32(uint32_t v) {
     asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(c), "+v"(d));
     return pick(c, d);
 }
-__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) { return wave_pick_u32<false>(v); }
 __device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
-    const uint32_t hi = wave_pick_u32<true>((uint32_t)(v >> 32));
-    const uint32_t lo = wave_pick_u32<true>((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0);
+    const uint32_t hi = wave_max_u32((uint32_t)(v >> 32));
+    const uint32_t lo = wave_max_u32((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0);
     return (uint64_t)hi << 32 | lo;
 }
 
@@ -413,13 +411,20 @@ __device__ __forceinline__ void put_steep(const Cut<T, align_for(TPR)>& cut, GT*
 }
 
 // Waves a SIMD is to hold (by the registers of NV packed vectors), and with them
-// the workgroups of a CU: the grid of the whole-row kernels.
-constexpr int waves_per_simd(int nv) { return nv <= 2 ? 8 : nv <= 8 ? 5 : 4; }
+// the workgroups of a CU: the grid of the whole-row kernels.  More of them hide the
+// sums of one row behind the loads of others, as far as the registers go without
+// spills in the loops (16384 rows of 50257 bf16, 13 vectors: six 284 us, four 306;
+// 65536 of 10000, 8 vectors: eight 332, five 359; with five alternatives and 4
+// vectors, 33554 rows of 4000 float: eight 120, seven 147; but with one and 13
+// vectors six, which spill, 401 and four 372).
+constexpr int waves_per_simd(int nv, bool grad, bool top) {
+    return nv <= 2 || (!grad && nv <= (top ? 4 : 8)) ? 8 : nv <= 8 ? 5 : !grad && !top && nv <= 13 ? 6 : 4;
+}
 
 // One workgroup per row or segment at a time, NV vectors per thread.  GT = void:
 // the forward; else the gradient too (whole rows).
 template <typename T, typename GT, int TPR, int NV, bool SEG, bool TOP>
-__global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(const LogprobArgs a, const LogprobGrad g, const SegArgs sg) {
+__global__ __launch_bounds__(TPR, waves_per_simd(NV, !std::is_void_v<GT>, TOP)) void k_token_logprobs(const LogprobArgs a, const LogprobGrad g, const SegArgs sg) {
     constexpr int V = kVec<T>;
     constexpr bool GRAD = !std::is_void_v<GT>;
     __shared__ RowShared<TPR, TOP> sh;
@@ -458,9 +463,6 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
         Top<TPR, TOP> top(sh, a.top_k);
         const int by = (int)((uint64_t)item % (TPR / 64));
         const auto edge_key = [&] { return has_edge ? order_key(edge, e0 + (uint32_t)cut.edge(tid)) : 0; };
-        // one wave takes few alternatives round by round; by the bound it costs some 1000
-        // instructions whatever their number
-        const bool by_rounds = TOP && TPR == 64 && a.top_k * (30 + 6 * NV * V) <= 1000;
         if constexpr (TOP) {
             __syncthreads();  // (the row before is done with the shared memory)
             const uint64_t kv = tid < cut.nv ? order_key(best, e0 + (uint32_t)cut.at(tid + bq * TPR)) : 0, ke = edge_key();
@@ -476,7 +478,7 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
             for (int w = 0; w < TPR / 64; ++w) m = fmaxf(m, sh.st.m[w]);
         }
         if constexpr (TOP) {
-            if (!by_rounds) top.bound(by);  // (the other waves go on)
+            top.bound(by);  // (the other waves go on)
         }
         const Scale scale(m);
         float s = 0.f, c = 0.f;
@@ -557,70 +559,38 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV)) void k_token_logprobs(cons
                 }
                 if (has_edge) f(edge_key());
             };
-            if (by_rounds) {
-                if (orderly) {
-                    // k times the largest below the last, by value and then index
-                    float last = INFINITY;
-                    uint32_t after = 0;  // of the last's value, only indices from here on
-                    for (int k = 0; k < a.top_k; ++k) {
-                        float b = -INFINITY;
-                        uint32_t at = ~0u;
-                        const auto take = [&](float v, uint32_t j, bool valid) {
-                            const bool left = valid && (v < last || (v == last && j >= after));
-                            const bool better = left && (v > b || at == ~0u || (v == b && j < at));
-                            b = better ? v : b;
-                            at = better ? j : at;
-                        };
+            const uint64_t bound = sh.top.bound;
+            if (orderly && top.mine >= bound) {
+                const float bv = bound > 1 ? key_value(bound) : -INFINITY;
+                uint32_t look = 0;  // vectors that may hold some of the best
 #pragma unroll
-                        for (int q = 0; q < NV; ++q) {
-                            float v[V];
-                            unpack(again(raw[q]), v);
-#pragma unroll
-                            for (int i = 0; i < V; ++i) take(v[i], (uint32_t)cut.at(tid + q * TPR) + i, tid + q * TPR < cut.nv);
-                        }
-                        take(edge, (uint32_t)cut.edge(tid), has_edge);
-                        last = wave_max(b);
-                        const uint32_t j = wave_min_u32(b == last ? at : ~0u);
-                        after = j + 1;
-                        if (tid == 0) emit(k, order_key(last, j));
-                    }
-                } else {
-                    top.finish(by, false, emit, each);
+                for (int q = 0; q < NV; ++q) {
+                    float v[V];
+                    unpack(again(raw[q]), v);
+                    look |= max_of(v) >= bv && tid + q * TPR < cut.nv ? 1u << q : 0;
                 }
-            } else {
-                const uint64_t bound = sh.top.bound;
-                if (orderly && top.mine >= bound) {
-                    const float bv = bound > 1 ? key_value(bound) : -INFINITY;
-                    uint32_t look = 0;  // vectors that may hold some of the best
+                for (; look; look &= look - 1) {
+                    const int w = __ffs(look) - 1;
+                    u32x4 one = raw[0];
 #pragma unroll
-                    for (int q = 0; q < NV; ++q) {
-                        float v[V];
-                        unpack(again(raw[q]), v);
-                        look |= max_of(v) >= bv && tid + q * TPR < cut.nv ? 1u << q : 0;
+                    for (int q = 1; q < NV; ++q) one = w == q ? raw[q] : one;
+                    float v[V];
+                    unpack(one, v);
+                    const uint32_t j = e0 + (uint32_t)cut.at(tid + w * TPR);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        // (by the vector's first index, as the bound: none of the best is lost)
+                        if (v[i] >= bv && order_key(v[i], j) >= bound) top.push(order_key(v[i], j + i));
                     }
-                    for (; look; look &= look - 1) {
-                        const int w = __ffs(look) - 1;
-                        u32x4 one = raw[0];
-#pragma unroll
-                        for (int q = 1; q < NV; ++q) one = w == q ? raw[q] : one;
-                        float v[V];
-                        unpack(one, v);
-                        const uint32_t j = e0 + (uint32_t)cut.at(tid + w * TPR);
-#pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            // (by the vector's first index, as the bound: none of the best is lost)
-                            if (v[i] >= bv && order_key(v[i], j) >= bound) top.push(order_key(v[i], j + i));
-                        }
-                    }
-                    const uint64_t ke = edge_key();
-                    if (ke >= bound) top.push(ke);
                 }
-                __syncthreads();
-                if constexpr (SEG) {
-                    if (tid >= cut.n && tid < a.top_k) sg.top[(r * a.top_k + tid) * sg.nseg + (item - r * sg.nseg)] = 0;
-                }
-                top.finish(by, orderly, emit, each);
+                const uint64_t ke = edge_key();
+                if (ke >= bound) top.push(ke);
             }
+            __syncthreads();
+            if constexpr (SEG) {
+                if (tid >= cut.n && tid < a.top_k) sg.top[(r * a.top_k + tid) * sg.nseg + (item - r * sg.nseg)] = 0;
+            }
+            top.finish(by, orderly, emit, each);
         }
 
         if constexpr (GRAD) {
@@ -826,7 +796,7 @@ void run_rows(const Plan& p, const LogprobArgs& a, const LogprobGrad& g, const S
     const int64_t items = a.rows * p.nseg;
 #define DART_ROW(TPR, NV)                                                                                        \
     if (p.tpr == TPR && p.nv == NV) {                                                                            \
-        const int64_t cap = (int64_t)device_cu_count() * (waves_per_simd(NV) * 256 / TPR);                        \
+        const int64_t cap = (int64_t)device_cu_count() * (waves_per_simd(NV, !std::is_void_v<GT>, TOP) * 256 / TPR); \
         k_token_logprobs<T, GT, TPR, NV, SEG, TOP><<<flat_grid(items < cap ? items : cap, TPR), TPR, 0, st>>>(a, g, sg); \
         return;                                                                                                  \
     }
