@@ -21,6 +21,8 @@
 #include "dart_common.hpp"
 #include "dart_internal.hpp"
 
+#include <algorithm>
+
 namespace dart {
 namespace {
 
@@ -414,48 +416,67 @@ __global__ __launch_bounds__(block_threads(TPR)) void k_layernorm_bwd(const Norm
 // grid is that, and a workgroup walks the rows.  More workgroups than that read
 // the weights again and leave a last round that is not full (16384 rows of 4096
 // bf16 with residual: forward 512 workgroups 80 us, 6.7 TB/s, 1024 85, one per
-// row 285; 32768 rows of 768 backward 768 workgroups 38 us, 5.3 TB/s, 512 44, 1024 47).
+// row 285; 32768 rows of 768 backward 768 workgroups 38 us, 5.3 TB/s, 512 44, 1024 47;
+// of 1280 forward 768 workgroups 30 us, 512 33).
 constexpr int waves_per_cu(bool bwd, int v, int e) {
-    return e <= 8 ? 16 : e <= 12 || (e == 16 && (v == 8 || !bwd)) ? 12 : 8;
+    return e <= 8 ? 16 : e <= 12 || (e == 24 && !bwd) || (e == 16 && (v == 8 || !bwd)) ? 12 : 8;
 }
 template <int TPR, int ITEMS, int V>
 unsigned blocks_for(bool bwd, int64_t rows) {
     constexpr int threads = block_threads(TPR), waves = threads / 64;
     const int64_t b = (rows + threads / TPR - 1) / (threads / TPR);
     const int per = waves_per_cu(bwd, V, ITEMS * V) / waves;
-    const int64_t cap = (int64_t)device_cu_count() * (per > 0 ? per : 1);
+    int64_t cap = (int64_t)device_cu_count() * (per > 0 ? per : 1);
+    // in the backward four rounds or more where two workgroups per CU are left: each
+    // ends in sums and a partial row (2048 rows of 2048 float 512 workgroups 19 us, 1024 24;
+    // 16384 of 64 float 8.3 and 9.8; but 256 where 512 are had, 8192 of 128 bf16, 9.6 and 8.3)
+    if (bwd && cap > b / 4) cap = std::min<int64_t>(cap, std::max<int64_t>(b / 4, 2 * (int64_t)device_cu_count()));
     return (unsigned)(b < cap ? b : cap);
 }
 // Most workgroups of any form of the backward: each leaves a partial row.
 int64_t bwd_cap() { return (int64_t)device_cu_count() * 4; }
 
-// The form that holds a row of n vectors: few idle lanes, few lanes to exchange
-// sums between, and at most 16 elements per lane (beyond that too few waves are
-// resident).  Backward of more than 8192 columns, 16 elements in each of 1024
-// lanes: the column sums stand in LDS (4096 rows of 16384 bf16 136 us, 4.0 TB/s; in
+// The form that holds a row of n vectors: few idle lanes, few lanes to exchange sums
+// between, and registers for two waves per SIMD.  A row to a wave needs no barrier: with
+// up to 24 elements per lane in the backward (32768 rows of 1280 bf16 55 us, 256 lanes to
+// a row 78; but 32, 8192 of 2048, 34.5 and 33.4) and 32 in the forward (32768 of 2048 bf16
+// 44.5 us, 6.0 TB/s, and 55), where there are rows for it (300 of 2048 4.3 and 3.5).
+// Float rows, with two vectors for one of bf16: up to 16 (100000 of 800, backward 182 and
+// 208, forward 119 and 131; 8192 of 2048 at 32 28.1 and 24.9).  Beyond that at most 16 per
+// lane.  Backward of more than 8192 columns, 16 elements in each of 1024
+// lanes: the column sums stand in LDS (4096 rows of 16384 bf16 with dsum 136 us, 4.0 TB/s; in
 // registers, spilt, 246).  Rows that are no multiple of a vector, at any alignment:
 // 16384 rows of 4095 bf16 forward 5.0 TB/s, of 4096 6.7 (element by element 1.5).
-#define DART_NORM_FORMS(V, F)                                        \
-    if constexpr (V == 8) {                                          \
-        if (n <= 16) F(8, 16, 1);                                    \
-        else if (n <= 64) F(8, 64, 1);                               \
-        else if (n <= 128) F(8, 64, 2);                              \
-        else if (n <= 256) F(8, 256, 1);                             \
-        else if (n <= 512) F(8, 512, 1);                             \
-        else if (n <= 1024) F(8, 1024, 1);                           \
-        else F(8, 1024, 2);                                          \
-    } else if constexpr (V == 4) {                                   \
-        if (n <= 16) F(4, 16, 1);                                    \
-        else if (n <= 64) F(4, 64, 1);                               \
-        else if (n <= 128) F(4, 64, 2);                              \
-        else if (n <= 192) F(4, 64, 3);                              \
-        else if (n <= 256) F(4, 256, 1);                             \
-        else if (n <= 512) F(4, 256, 2);                             \
-        else if (n <= 1024) F(4, 512, 2);                            \
-        else if (n <= 2048) F(4, 1024, 2);                           \
-        else F(4, 1024, 4);                                          \
-    } else {                                                         \
-        F(1, 16, 1); /* rows of less than one vector */              \
+#define DART_NORM_FORMS(V, BWD, FEW, F)                 \
+    if constexpr (V == 8) {                             \
+        if (n <= 16) F(8, 16, 1);                       \
+        else if (n <= 64) F(8, 64, 1);                  \
+        else if (n <= 128) F(8, 64, 2);                 \
+        else if (n <= 192 && !(FEW)) F(8, 64, 3);       \
+        else if (n <= 256) {                            \
+            if constexpr (BWD) F(8, 256, 1);            \
+            else if (FEW) F(8, 256, 1);                 \
+            else F(8, 64, 4);                           \
+        }                                               \
+        else if (n <= 512) F(8, 512, 1);                \
+        else if (n <= 1024) F(8, 1024, 1);              \
+        else F(8, 1024, 2);                             \
+    } else if constexpr (V == 4) {                      \
+        if (n <= 16) F(4, 16, 1);                       \
+        else if (n <= 64) F(4, 64, 1);                  \
+        else if (n <= 128) F(4, 64, 2);                 \
+        else if (n <= 192) F(4, 64, 3);                 \
+        else if (n <= 256) {                            \
+            if constexpr (BWD) F(4, 64, 4);             \
+            else if (FEW) F(4, 256, 1);                 \
+            else F(4, 64, 4);                           \
+        }                                               \
+        else if (n <= 512) F(4, 256, 2);                \
+        else if (n <= 1024) F(4, 512, 2);               \
+        else if (n <= 2048) F(4, 1024, 2);              \
+        else F(4, 1024, 4);                             \
+    } else {                                            \
+        F(1, 16, 1); /* rows of less than one vector */ \
     }
 
 template <typename T, int V>
@@ -465,7 +486,8 @@ void run_layernorm(const NormArgs& a, hipStream_t st) {
     a.D % V_ == 0                                                                                                       \
         ? k_layernorm<T, V_, TPR, ITEMS, false><<<blocks_for<TPR, ITEMS, V_>(false, a.rows), block_threads(TPR), 0, st>>>(a) \
         : k_layernorm<T, V_, TPR, ITEMS, true><<<blocks_for<TPR, ITEMS, V_>(false, a.rows), block_threads(TPR), 0, st>>>(a)
-    DART_NORM_FORMS(V, DART_F)
+    const bool few = a.rows < 4 * (int64_t)device_cu_count();
+    DART_NORM_FORMS(V, false, few, DART_F)
 #undef DART_F
 }
 
@@ -478,7 +500,7 @@ unsigned run_layernorm_bwd(const NormBwdArgs& a, hipStream_t st) {
     (blocks = blocks_for<TPR, ITEMS, V_>(true, a.rows),                                               \
      a.D % V_ == 0 ? k_layernorm_bwd<T, GT, V_, TPR, ITEMS, false><<<blocks, block_threads(TPR), 0, st>>>(a) \
                    : k_layernorm_bwd<T, GT, V_, TPR, ITEMS, true><<<blocks, block_threads(TPR), 0, st>>>(a))
-    DART_NORM_FORMS(V, DART_F)
+    DART_NORM_FORMS(V, true, false, DART_F)
 #undef DART_F
     return blocks;
 }

@@ -273,3 +273,20 @@ def test_other_stream_and_device_checks():
         dart.layernorm(x[:1].expand(500, 768), w)
     with pytest.raises(dart.DartError):
         dart.layernorm_bwd(x.float(), dout, w)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [1000, 1030, 1500, 1536, 1700, 2047, 2048])
+def test_many_rows_of_a_wave(dtype, D):
+    """Enough rows for a wave each, and for workgroups of several rounds."""
+    rng = np.random.default_rng(D)
+    for rows in (1024, 4100):
+        print("\n[gpu-case] norm %s rows=%d D=%d" % (dtype, rows, D), flush=True)
+        x, res = tensor(rand(rng, rows, D, shift=0.5), dtype), tensor(rand(rng, rows, D), dtype)
+        w, b = tensor(1 + 0.2 * rand(rng, D), "fp32"), tensor(rand(rng, D), "fp32")
+        out, total = dart.layernorm(x, w, b, residual=res, eps=EPS)
+        s, dev, inv = check_forward(x, res, w, b, True, dtype, out, total)
+        for gdtype in {"fp32", dtype}:
+            dout, dsum = tensor(rand(rng, rows, D), gdtype), tensor(rand(rng, rows, D), gdtype)
+            g = dart.layernorm_bwd(total, dout, w, dsum=dsum, eps=EPS, want_bias=True)
+            check_backward(s, dev, inv, w, True, dout, dsum, g, gdtype)
