@@ -437,8 +437,8 @@ dart_status dart_token_logprobs_bwd(int64_t rows, int64_t vocab, int64_t row_str
  * dart_token_logprobs_grad: the forward and that gradient in one call, for a
  * loss whose dlogprob, dentropy and dlse are known before (a mean over the
  * tokens, say): the logits are read from memory once where a row fits a
- * workgroup's registers.  Arguments as above; row_max, log_sum and, with dentropy, entropy must
- * be given; dlogits may be logits itself.
+ * workgroup's registers.  Arguments as above; row_max, log_sum and, with
+ * dentropy, entropy must be given; dlogits may be logits itself.
  */
 dart_status dart_token_logprobs_grad(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
                                      int32_t grad_dtype, const void* logits, const int64_t* targets,
