@@ -834,6 +834,7 @@ void run_bwd(const LogprobArgs& a, const LogprobGrad& g, hipStream_t st) {
 
 size_t token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int dtype, int top_k) {
     size_t need = 0;
+    if (rows == 0) return need;
     for (const bool grad : {false, true}) {
         const Plan p = plan_for(rows, vocab, dtype, top_k, grad);
         if (p.nseg > 1) {

@@ -458,3 +458,22 @@ def test_masked_logits_stay_without_gradient(V, R):
         masked = torch.isneginf(l)
         masked[0, 1] = False   # the first row's target keeps its own term
         assert not bool(g[masked].any())
+
+
+@pytest.mark.parametrize("V", [50, 2049, 50257, 200001])
+def test_an_empty_batch_of_any_vocabulary(V):
+    """What a mask that selects no token leaves."""
+    import torch
+    from paper_2608_02032_amd import layer
+    z, none = torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        l = torch.randn(3, V, device="cuda").to(dtype)[torch.zeros(3, dtype=torch.bool, device="cuda")].requires_grad_()
+        e = l.detach()
+        r = dart.token_logprobs(e, z, top_k=3)
+        assert r["logprob"].shape == (0,) and r["top_ids"].shape == (0, 3)
+        assert dart.token_logprobs_bwd(e, r["row_max"], r["log_sum"], targets=z, dlogprob=none).shape == (0, V)
+        assert dart.token_logprobs_grad(e, z, none)["dlogits"].shape == (0, V)
+        lp, ent = layer.token_logprobs(l, z)
+        (lp.sum() + ent.sum()).backward()
+        assert l.grad.shape == (0, V)
+    torch.cuda.synchronize()

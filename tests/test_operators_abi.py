@@ -183,3 +183,15 @@ def test_row_strides_and_dense_tensors():
     assert dart._row_stride(a[:, 0, :].expand(6, 16)[:1].expand(4, 16), "a") == 0   # refused by the library
     assert dart._dense(a.transpose(0, 2)) and dart._dense(a[2:4]) and dart._dense(torch.zeros(0, 3).t())
     assert not dart._dense(a[:, :4]) and not dart._dense(a[0, :1].expand(3, 16)) and not dart._dense(a[:, ::2].transpose(0, 1))
+
+
+@pytest.mark.parametrize("vocab", [1, 2048, 2049, 50257, 131073, 1 << 24])
+def test_no_rows_need_no_workspace(lib, vocab):
+    for dtype in (F32, BF16):
+        for k in (0, 1):
+            assert lib.dart_token_logprobs_workspace_bytes(0, vocab, dtype, k) == 0
+    # past every check there is nothing to launch
+    assert lp(lib, rows=0, vocab=vocab, stride=vocab, k=0, logits=None, targets=None, logprob=None, ids=None, tops=None, ws=None,
+              nbytes=0) == 0
+    assert lp_bwd(lib, rows=0, vocab=vocab, stride=vocab, ds=vocab) == 0
+    assert lp_grad(lib, rows=0, vocab=vocab, stride=vocab, ds=vocab) == 0
