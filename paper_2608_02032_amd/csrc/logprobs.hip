@@ -86,11 +86,11 @@ __device__ __forceinline__ float wave_max(float v) {
 }
 
 // Order of the alternatives: by value (a NaN above all, -0 as 0), then by the
-// lowest index; as one integer, larger first, never 0.
+// lowest index; as one integer, larger first, never 0 and never all ones.
 __device__ __forceinline__ uint64_t order_key(float v, uint32_t index) {
     const float z = v + 0.f;
     uint32_t u = __builtin_bit_cast(uint32_t, z);
-    u = z != z ? 0xFFFFFFFFu : (u >> 31 ? ~u : u | 0x80000000u);
+    u = z != z ? 0xFFFFFFFEu : (u >> 31 ? ~u : u | 0x80000000u);
     return (uint64_t)u << 32 | (uint32_t)~index;
 }
 __device__ __forceinline__ float key_value(uint64_t key) {

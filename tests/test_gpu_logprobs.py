@@ -477,3 +477,26 @@ def test_an_empty_batch_of_any_vocabulary(V):
         (lp.sum() + ent.sum()).backward()
         assert l.grad.shape == (0, V)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V,R", [(1, 3), (4, 3), (33, 3), (600, 3), (5000, 3), (50257, 2), (50257, 300), (200001, 2)])
+def test_nan_is_above_all_wherever_it_is(dtype, V, R):
+    """NaN first, by the lowest index, then the others: at column 0 too, in whole rows and in segments, in rows of
+    nothing else, and where every token is among the alternatives."""
+    print("\n[gpu-case] logprobs NaN order %s V=%d R=%d" % (dtype, V, R), flush=True)
+    rng = np.random.default_rng(V)
+    sets = [[0], [0, V - 1], [V // 2], [0, V // 3, V // 2], list(range(V)), list(range(0, V, 7))]
+    a = np.round(rng.standard_normal((R, V)) * 20) / 4   # quarters: the same in bfloat16, and many ties
+    if V > 1:
+        a[:, V // 5] = np.inf
+    for r in range(R):
+        a[r, sets[r % len(sets)]] = np.nan
+    for k in sorted({1, min(V, 4), min(V, 32)}):
+        r = dart.token_logprobs(tensor(a, dtype), top_k=k)
+        order = np.argsort(np.where(np.isnan(a), -np.inf, -a), axis=1, kind="stable")
+        # (a stable sort: of the NaN, which share their key with +infinity, those first)
+        want = np.stack([np.concatenate([np.flatnonzero(np.isnan(x)), o[~np.isnan(x[o])]])[:k] for x, o in zip(a, order)])
+        assert np.array_equal(r["top_ids"].cpu().numpy(), want)
+        one = dart.token_logprobs_grad(tensor(a, dtype), ids(np.zeros(R)), tensor(np.ones(R)), top_k=k)
+        assert np.array_equal(one["top_ids"].cpu().numpy(), want)
