@@ -525,6 +525,8 @@ __global__ __launch_bounds__(TPR, waves_per_simd(NV, !std::is_void_v<GT>, TOP)) 
                 s += sh.st.s[w];
                 c += sh.st.c[w];
             }
+        } else if constexpr (TOP) {
+            __syncthreads();  // (the bound; the waves' sums give larger workgroups theirs)
         }
         const float scaled_sum = s;
         {

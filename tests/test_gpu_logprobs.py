@@ -500,3 +500,20 @@ def test_nan_is_above_all_wherever_it_is(dtype, V, R):
         assert np.array_equal(r["top_ids"].cpu().numpy(), want)
         one = dart.token_logprobs_grad(tensor(a, dtype), ids(np.zeros(R)), tensor(np.ones(R)), top_k=k)
         assert np.array_equal(one["top_ids"].cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [9, 40, 64, 200, 257, 600, 1000, 2000])
+def test_alternatives_of_rows_of_one_wave(dtype, V):
+    """Rows that a wave holds, one after the other in the same shared memory, with bounds that one lane finds (more
+    than eight alternatives) and that all do: every row's own alternatives."""
+    import torch
+    print("\n[gpu-case] logprobs one wave %s V=%d" % (dtype, V), flush=True)
+    rng = np.random.default_rng(V)
+    a = np.round(rng.standard_normal((20000, V)) * 20) / 4
+    l = tensor(a, dtype)
+    order = torch.sort(l, dim=1, descending=True, stable=True).indices
+    for k in sorted({min(V, n) for n in (1, 8, 9, 16, 32)}):
+        assert dart.token_logprobs(l, top_k=k)["top_ids"].equal(order[:, :k]), k
+        one = dart.token_logprobs_grad(l, torch.zeros(len(a), dtype=torch.int64, device="cuda"), torch.ones(len(a), device="cuda"), top_k=k)
+        assert one["top_ids"].equal(order[:, :k]), k
