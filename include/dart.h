@@ -455,7 +455,8 @@ dart_status dart_token_logprobs_grad(int64_t rows, int64_t vocab, int64_t row_st
  *   out_i = g_i scale c,   c = min(1, max_norm / (norm + 1e-6)).
  * The squares are summed in 64 bits.  A NaN among the gradients makes norm and
  * every out NaN; an infinity makes c = 0 (and itself NaN).  max_norm may be
- * infinite (scaling alone).  dart_grad_norm computes norm alone.
+ * infinite: scaling alone, c = 1 for an infinite norm too.  dart_grad_norm
+ * computes norm alone.
  *   grads, outs  HOST arrays of n device pointers; numels HOST array of n
  *                element counts (0 allowed: the pointers are not used);
  *                dtypes, out_dtypes HOST arrays of n dart_dtypes.  The arrays

@@ -1,6 +1,6 @@
 // clip.hip -- the global norm of many gradient tensors and their clipping:
 //   n = scale sqrt(sum over all tensors of sum g^2),
-//   c = min(1, max_norm / (n + 1e-6)),   out = g scale c.
+//   c = min(1, max_norm / (n + 1e-6)) (1 without a limit),   out = g scale c.
 // The squares are formed and summed in 64 bits: the square of no float
 // overflows or underflows there, and sums over 10^9 elements keep their digits.
 // The order is fixed (no atomics).
@@ -189,7 +189,8 @@ __global__ __launch_bounds__(kThreads) void k_clip(const Batch b, const Entry* t
     for (int i = threadIdx.x; i < nparts; i += kThreads) acc += part[i];
     const double total = fabs((double)scale) * sqrt(block_sum64(acc, s_red));
     if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = (float)total;
-    const double coef = (double)max_norm / (total + 1e-6);
+    // (no limit, no clipping: an infinite norm would make inf / inf of it)
+    const double coef = max_norm == INFINITY && total == total ? 1.0 : (double)max_norm / (total + 1e-6);
     const float f = (float)(scale * (coef >= 1.0 ? 1.0 : coef));  // (a NaN stays)
     const int64_t c0 = chunks * blockIdx.x / gridDim.x, c1 = chunks * (blockIdx.x + 1) / gridDim.x;
     if (c0 == c1) return;

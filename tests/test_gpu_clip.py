@@ -172,3 +172,21 @@ def test_within_the_limit_nothing_is_written_and_streams():
         junk = [torch.full((1 << 14,), 3.0, device="cuda") for _ in range(8)]
     side.synchronize()
     assert norm.equal(ref) and junk
+
+
+@pytest.mark.parametrize("to", ["", "fp32", "bf16"])
+def test_an_infinite_limit_scales_whatever_the_norm(to):
+    """An infinity among the gradients, without a limit: the others are scaled, not lost; a NaN still spoils all."""
+    import torch
+    for dtype in ("fp32", "bf16"):
+        g = [tensor(np.arange(5000) % 7, dtype), tensor(np.ones(10), "fp32")]
+        g[1][3] = float("inf")
+        before = [f64(t) for t in g]
+        out = [torch.full(t.shape, 7.0, dtype=tdtype(to), device="cuda") for t in g] if to else None
+        n = dart.clip_grad_norm(g, float("inf"), scale=0.5, out=out)
+        assert float(n) == float("inf")
+        for b, o in zip(before, g if out is None else out):
+            assert np.array_equal(f64(o), 0.5 * b)   # (halves of small whole numbers: exact)
+        g = [torch.ones(500, device="cuda"), torch.ones(10, device="cuda")]
+        g[1][3] = float("nan")
+        assert bool(torch.isnan(dart.clip_grad_norm(g, float("inf")))) and all(bool(torch.isnan(t).all()) for t in g)
