@@ -133,6 +133,15 @@ struct RowSum {
     }
 };
 
+// sum / d with inv_d the nearest to 1 / d: the product corrected once by its remainder
+// (the step of a division after Markstein), which is the quotient itself where that is a
+// float.  The product alone is off by a step or so of a mean that every deviation is
+// taken from: in a row of 300 in 4095 columns 3e-5 of deviation where there is none.
+__device__ __forceinline__ float mean_of(float sum, int d, float inv_d) {
+    const float q = sum * inv_d;
+    return __builtin_fmaf(__builtin_fmaf(-q, (float)d, sum), inv_d, q);
+}
+
 constexpr int block_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 
 // The row of a workgroup's rows at a time that a lane works on, as a scalar where
@@ -214,7 +223,7 @@ __global__ __launch_bounds__(block_threads(TPR)) void k_layernorm(const NormArgs
         float mu = 0.f, ss[1] = {0.f};
         if (a.center) {
             row_sum(m);
-            mu = m[0] * a.inv_d;
+            mu = mean_of(m[0], a.D, a.inv_d);
         }
 #pragma unroll
         for (int q = 0; q < ITEMS; ++q) {
@@ -309,7 +318,7 @@ __global__ __launch_bounds__(block_threads(TPR)) void k_layernorm_bwd(const Norm
         if constexpr (ahead) load(r + step);
         if (a.center) {
             row_sum(m);
-            const float mu = m[0] * a.inv_d;
+            const float mu = mean_of(m[0], a.D, a.inv_d);
 #pragma unroll
             for (int q = 0; q < ITEMS; ++q) {
 #pragma unroll

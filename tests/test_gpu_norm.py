@@ -290,3 +290,48 @@ def test_many_rows_of_a_wave(dtype, D):
             dout, dsum = tensor(rand(rng, rows, D), gdtype), tensor(rand(rng, rows, D), gdtype)
             g = dart.layernorm_bwd(total, dout, w, dsum=dsum, eps=EPS, want_bias=True)
             check_backward(s, dev, inv, w, True, dout, dsum, g, gdtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [3, 100, 1000, 1001, 1500, 2047, 4095, 5000, 8191, 12289, 16384])
+def test_constant_rows_of_any_width(dtype, D):
+    """A row of one value has no deviation: out = bias to the last bit, xh = 0 and inv = eps^-1/2.  Of values of eight
+    bits every partial sum of up to 2^14 has 22 and is exact in float, so that only the division could round."""
+    rng = np.random.default_rng(D)
+    print("\n[gpu-case] norm constant rows %s D=%d" % (dtype, D), flush=True)
+    c = np.array([300.0, 2.5, 3.0, 0.1, -1234.5, 1.0 / 3.0, 0.0, 77.7])
+    x = tensor(f64(tensor(np.repeat(c[:, None], D, 1), "bf16")), dtype)
+    w, b = tensor(rand(rng, D), "fp32"), tensor(rand(rng, D), "fp32")
+    out = dart.layernorm(x, w, b, eps=EPS)
+    want = b.to(x.dtype).double().cpu().numpy()
+    assert np.array_equal(f64(out), np.broadcast_to(want, out.shape))
+    zero = x.new_zeros(x.shape)
+    assert np.array_equal(f64(dart.layernorm(x, w, b, residual=zero, eps=EPS)[0]), np.broadcast_to(want, out.shape))
+    for gdtype in {"fp32", dtype}:
+        dout = tensor(rand(rng, len(c), D), gdtype)
+        g = dart.layernorm_bwd(x, dout, w, eps=EPS, want_bias=True)
+        inv = 1 / np.sqrt(EPS)
+        gw = f64(dout) * f64(w)
+        dx = inv * (gw - gw.mean(-1, keepdims=True))
+        # the sum of the gradients (fewer than 64 roundings along a path) and the formula's few
+        bound = 2 * 64 * U * inv * np.abs(gw).max(-1, keepdims=True)
+        within(g["dx"], dx, STEP[gdtype] * np.abs(dx) + bound, "dx")
+        assert not bool(g["dweight"].any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [1000, 4095, 16384])
+def test_small_deviations_from_a_large_mean(dtype, D):
+    """Rows that leave one value by a step of bfloat16 in places (sums exact, as above): out is off by the mean's one
+    rounding, u |c| inv, and by the mean square's (fewer than 64 along a path): 128 u of the row's largest."""
+    rng = np.random.default_rng(D + 1)
+    print("\n[gpu-case] norm small deviations %s D=%d" % (dtype, D), flush=True)
+    c = np.array([300.0, 3.0, -40.0, 1000.0])[:, None]
+    a = np.broadcast_to(c, (4, D)) * (1 + (rng.random((4, D)) < 0.2) * 2.0 ** -7)
+    x = tensor(f64(tensor(a, "bf16")), dtype)
+    w = tensor(1 + 0.1 * rand(rng, D), "fp32")
+    for center in (True, False):
+        s, dev, inv, ref = reference(x, None, w, None, center, dtype)
+        bound = 2 * U * np.abs(s).max(-1, keepdims=True) * inv + 128 * U * np.abs(dev * inv).max(-1, keepdims=True)
+        bound = STEP[dtype] * np.abs(ref) + bound * float(w.max())
+        within(dart.layernorm(x, w, eps=EPS, center=center), ref, bound, "out")
