@@ -402,6 +402,7 @@ dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t
  *   <= min(vocab, DART_MAX_TOP_K), the pointers NULL where top_k = 0
  *   workspace  device buffer of >= dart_token_logprobs_workspace_bytes() (may
  *   be NULL where that is 0)
+ * A result (or the workspace) that overlaps another argument is refused.
  */
 #define DART_MAX_TOP_K 32
 size_t dart_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t dtype, int32_t top_k);
@@ -423,7 +424,7 @@ dart_status dart_token_logprobs(int64_t rows, int64_t vocab, int64_t row_stride,
  *   dlogits [rows][dlogits_row_stride] grad_dtype: DART_FP32, or DART_BF16 with
  *   bf16 logits; elements past vocab of a row are left as they are
  * dlogits may be logits itself (the same pointer, type and stride); any other
- * overlap is refused.
+ * overlap of dlogits is refused.
  */
 dart_status dart_token_logprobs_bwd(int64_t rows, int64_t vocab, int64_t row_stride, int32_t dtype,
                                     int32_t grad_dtype, const void* logits, const int64_t* targets,
@@ -466,6 +467,7 @@ dart_status dart_token_logprobs_grad(int64_t rows, int64_t vocab, int64_t row_st
  *                are refused.  Any alignment of whole elements.
  *   norm         device [1] float
  *   workspace    device buffer of >= dart_grad_norm_workspace_bytes(n)
+ * norm and the workspace overlap nothing else (refused).
  */
 size_t dart_grad_norm_workspace_bytes(int64_t n);
 dart_status dart_grad_norm(int64_t n, const void* const* grads, const int64_t* numels,

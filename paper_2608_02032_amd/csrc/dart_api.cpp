@@ -12,6 +12,7 @@
 #include <cstdio>
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 
 #include "dart_internal.hpp"
@@ -98,8 +99,24 @@ struct Range {
     uintptr_t a, b;  // first byte, one past the last
     Range(const void* p, int64_t rows, int64_t stride, int64_t width, int dtype)
         : a((uintptr_t)p), b(p && rows > 0 ? a + (uintptr_t)((rows - 1) * stride + width) * dart::elem_bytes(dtype) : a) {}
-    bool meets(const Range& o) const { return a < o.b && o.a < b; }
+    Range(const void* p, size_t bytes) : a((uintptr_t)p), b(p ? a + bytes : a) {}
+    bool meets(const Range& o) const { return a < o.b && o.a < b && a < b && o.a < o.b; }
 };
+
+// What is written meets nothing that is read and nothing else that is written.
+struct Named {
+    const char* name;
+    Range r;
+};
+dart_status check_apart(std::initializer_list<Named> written, std::initializer_list<Named> read) {
+    for (const Named* w = written.begin(); w != written.end(); ++w) {
+        for (const Named* o = written.begin(); o != w; ++o)
+            if (w->r.meets(o->r)) return fail(DART_ERR_INVALID_ARG, "%s overlaps %s", w->name, o->name);
+        for (const Named& o : read)
+            if (w->r.meets(o.r)) return fail(DART_ERR_INVALID_ARG, "%s overlaps %s", w->name, o.name);
+    }
+    return DART_OK;
+}
 
 // rows x stride elements have to be addressable.
 bool too_large(int64_t rows, int64_t stride) { return rows > 0 && stride > ((int64_t)1 << 56) / rows; }
@@ -477,6 +494,7 @@ dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t
     if (st != DART_OK) return st;
     st = check_dtypes(dtype, grad_dtype);
     if (st != DART_OK) return st;
+    const size_t need = dart::layernorm_bwd_workspace_bytes(rows, dim);
     if (rows > 0) {
         REQUIRE_PTR(x);
         REQUIRE_PTR(dout);
@@ -492,8 +510,10 @@ dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t
             if (o->meets(rx) || o->meets(ro) || o->meets(rs) || o->meets(rd) || o->meets(rw))
                 return fail(DART_ERR_INVALID_ARG, "dweight or dbias overlaps another argument");
         if (rdw.meets(rdb)) return fail(DART_ERR_INVALID_ARG, "dweight overlaps dbias");
+        st = check_apart({{"workspace", Range(workspace, need)}},
+                         {{"x", rx}, {"weight", rw}, {"dout", ro}, {"dsum", rs}, {"dx", rd}, {"dweight", rdw}, {"dbias", rdb}});
+        if (st != DART_OK) return st;
     }
-    const size_t need = dart::layernorm_bwd_workspace_bytes(rows, dim);
     if (workspace_bytes < need)
         return fail(DART_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
     if (workspace && (uintptr_t)workspace % 16 != 0)
@@ -532,6 +552,10 @@ static dart_status check_dlogits(int64_t rows, int64_t vocab, int64_t row_stride
     return DART_OK;
 }
 
+// `n` values of the rows' results or weights.
+static Range of_rows(const float* p, int64_t n) { return Range(p, (size_t)n * sizeof(float)); }
+static Range of_rows(const int64_t* p, int64_t n) { return Range(p, (size_t)n * sizeof(int64_t)); }
+
 size_t dart_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t dtype, int32_t top_k) {
     if (check_logits(rows, vocab, vocab, dtype, DART_FP32, top_k) != DART_OK) return 0;
     return dart::token_logprobs_workspace_bytes(rows, vocab, dtype, top_k);
@@ -552,6 +576,20 @@ static dart_status run_token_logprobs(const dart::LogprobArgs& a, const dart::Lo
         return fail(DART_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
     if (workspace && (uintptr_t)workspace % 16 != 0)
         return fail(DART_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const int64_t n = a.rows, k = a.rows * a.top_k;
+    const dart::LogprobGrad g = grad ? *grad : dart::LogprobGrad{};
+    const Range dlogits(g.dlogits, n, g.stride, a.vocab, g.dtype);
+    // (dlogits against logits has rules of its own)
+    dart_status st = check_apart(
+        {{"logprob", of_rows(a.logprob, n)}, {"entropy", of_rows(a.entropy, n)}, {"row_max", of_rows(a.row_max, n)},
+         {"log_sum", of_rows(a.log_sum, n)}, {"top_ids", of_rows(a.top_ids, k)}, {"top_logprobs", of_rows(a.top_logprobs, k)},
+         {"workspace", Range(workspace, need)}},
+        {{"logits", Range(a.logits, n, a.stride, a.vocab, a.dtype)}, {"targets", of_rows(a.targets, n)},
+         {"dlogprob", of_rows(g.dlogprob, n)}, {"dentropy", of_rows(g.dentropy, n)}, {"dlse", of_rows(g.dlse, n)}, {"dlogits", dlogits}});
+    if (st == DART_OK)
+        st = check_apart({{"dlogits", dlogits}}, {{"targets", of_rows(a.targets, n)}, {"dlogprob", of_rows(g.dlogprob, n)},
+                                                  {"dentropy", of_rows(g.dentropy, n)}, {"dlse", of_rows(g.dlse, n)}});
+    if (st != DART_OK) return st;
     return hip_status(dart::launch_token_logprobs(a, grad, workspace, (hipStream_t)stream), what);
 }
 
@@ -585,6 +623,11 @@ dart_status dart_token_logprobs_bwd(int64_t rows, int64_t vocab, int64_t row_str
     REQUIRE_PTR(log_sum);
     REQUIRE_PTR(dlogits);
     if (dentropy && !entropy) return fail(DART_ERR_INVALID_ARG, "dentropy needs entropy");
+    st = check_apart({{"dlogits", Range(dlogits, rows, dlogits_row_stride, vocab, grad_dtype)}},
+                     {{"targets", of_rows(targets, rows)}, {"row_max", of_rows(row_max, rows)}, {"log_sum", of_rows(log_sum, rows)},
+                      {"entropy", of_rows(entropy, rows)}, {"dlogprob", of_rows(dlogprob, rows)},
+                      {"dentropy", of_rows(dentropy, rows)}, {"dlse", of_rows(dlse, rows)}});
+    if (st != DART_OK) return st;
     const dart::LogprobArgs a{rows, vocab, row_stride, dtype, 0, logits, targets, ignore_index,
                               nullptr, const_cast<float*>(entropy), const_cast<float*>(row_max),
                               const_cast<float*>(log_sum), nullptr, nullptr};
@@ -630,6 +673,8 @@ static dart_status check_grads(int64_t n, const void* const* grads, void* const*
         return fail(DART_ERR_INVALID_ARG, "workspace too small: %zu < %zu bytes", workspace_bytes,
                     dart::grad_norm_workspace_bytes(n));
     if ((uintptr_t)workspace % 16 != 0) return fail(DART_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const Range rn(norm, sizeof(float)), rws(workspace, dart::grad_norm_workspace_bytes(n));
+    if (rn.meets(rws)) return fail(DART_ERR_INVALID_ARG, "norm overlaps workspace");
     if (n == 0) return DART_OK;
     REQUIRE_PTR(grads);
     REQUIRE_PTR(numels);
@@ -646,6 +691,10 @@ static dart_status check_grads(int64_t n, const void* const* grads, void* const*
         if ((uintptr_t)grads[i] % dart::elem_bytes(dtypes[i]) != 0 ||
             (outs && (uintptr_t)outs[i] % dart::elem_bytes(out_dtypes[i]) != 0))
             return fail(DART_ERR_INVALID_ARG, "tensor %lld: not aligned to its elements", (long long)i);
+        const Range g(grads[i], 1, 0, numels[i], dtypes[i]);
+        const Range o = outs ? Range(outs[i], 1, 0, numels[i], out_dtypes[i]) : g;
+        if (g.meets(rn) || g.meets(rws) || o.meets(rn) || o.meets(rws))
+            return fail(DART_ERR_INVALID_ARG, "tensor %lld: overlaps norm or workspace", (long long)i);
     }
     if (!outs) return DART_OK;
     // Whatever is written may meet nothing else: the ranges in order of their

@@ -195,3 +195,59 @@ def test_no_rows_need_no_workspace(lib, vocab):
               nbytes=0) == 0
     assert lp_bwd(lib, rows=0, vocab=vocab, stride=vocab, ds=vocab) == 0
     assert lp_grad(lib, rows=0, vocab=vocab, stride=vocab, ds=vocab) == 0
+
+
+def test_norm_backward_refuses_a_workspace_in_its_arguments(lib):
+    need = lib.dart_layernorm_bwd_workspace_bytes(4, 64)
+    for k in range(1, 8):
+        # it ends inside the argument at k P, or begins there
+        assert norm_bwd(lib, ws=k * P) == INVALID and b"workspace overlaps" in lib.dart_last_error()
+        assert norm_bwd(lib, ws=k * P - need + 16) == INVALID and b"workspace overlaps" in lib.dart_last_error()
+
+
+LP = dict(logits=P, targets=2 * P, dlp=3 * P, dent=4 * P, dlse=5 * P, logprob=6 * P, ent=7 * P, m=8 * P, ls=9 * P, ids=10 * P,
+          tops=11 * P, dl=12 * P, ws=14 * P)
+
+
+def lp_apart(lib, one_call, rows=2, vocab=200000, k=3, **kw):
+    a = dict(LP, **kw)
+    need = lib.dart_token_logprobs_workspace_bytes(rows, vocab, BF16, k)
+    assert need > 0
+    if one_call:
+        return lib.dart_token_logprobs_grad(rows, vocab, vocab, BF16, BF16, a["logits"], a["targets"], -100, k, a["dlp"], a["dent"],
+                                            a["dlse"], a["logprob"], a["ent"], a["m"], a["ls"], a["ids"], a["tops"], a["dl"], vocab,
+                                            a["ws"], need, None)
+    return lib.dart_token_logprobs(rows, vocab, vocab, BF16, a["logits"], a["targets"], -100, k, a["logprob"], a["ent"], a["m"],
+                                   a["ls"], a["ids"], a["tops"], a["ws"], need, None)
+
+
+@pytest.mark.parametrize("one_call", [False, True])
+@pytest.mark.parametrize("name", ["logprob", "ent", "m", "ls", "ids", "tops", "ws"])
+def test_token_logprobs_results_meet_nothing_else(lib, one_call, name):
+    others = [n for n in LP if n != name and (one_call or n not in ("dlp", "dent", "dlse", "dl"))]
+    for other in others:
+        assert lp_apart(lib, one_call, **{name: LP[other]}) == INVALID and b"overlaps" in lib.dart_last_error(), other
+    # the last byte of the logits and, in the one call, of their gradient
+    end = 2 * 200000 * 2
+    assert lp_apart(lib, one_call, **{name: P + end - 16}) == INVALID and b"overlaps" in lib.dart_last_error()
+    if one_call:
+        assert lp_apart(lib, True, **{name: 12 * P + end - 16}) == INVALID and b"overlaps" in lib.dart_last_error()
+
+
+def test_gradient_of_the_logits_meets_no_input(lib):
+    for other in ("targets", "dlp", "dent", "dlse"):
+        assert lp_apart(lib, True, dl=LP[other]) == INVALID and b"dlogits" in lib.dart_last_error()
+    for k in range(2, 8):
+        assert lp_bwd(lib, dl=k * P) == INVALID and b"dlogits" in lib.dart_last_error()
+        assert lp_bwd(lib, dl=k * P - 2 * 400 + 2) == INVALID and b"dlogits" in lib.dart_last_error()
+
+
+@pytest.mark.parametrize("reads_only", [False, True])
+def test_norm_and_workspace_lie_in_no_tensor(lib, reads_only):
+    need = lib.dart_grad_norm_workspace_bytes(2)
+    for kw in (dict(norm=P), dict(norm=P + 396), dict(norm=2 * P + 96), dict(ws=P), dict(ws=2 * P + 96), dict(ws=P - need + 16),
+               dict(norm=10 * P), dict(norm=10 * P + need - 4)):
+        assert clip(lib, reads_only=reads_only, **kw) == INVALID and b"overlaps" in lib.dart_last_error(), kw
+    if not reads_only:
+        for kw in (dict(norm=3 * P + 8), dict(ws=4 * P)):
+            assert clip(lib, outs=(3 * P, 4 * P), **kw) == INVALID and b"overlaps" in lib.dart_last_error(), kw
