@@ -722,7 +722,8 @@ def _token_logprobs(logits, targets, top_k, ignore_index, stream, grad=None):
             _same(grad[k], lead, torch.float32, k)
     empty = _allocator(stream)
     rows_out = empty((4,) + lead, dtype=torch.float32, device=device)
-    logprob, entropy, row_max, log_sum = rows_out.unbind(0)
+    # (.data: each a tensor of its own to autograd, which would take a change of one in place for a change of all)
+    logprob, entropy, row_max, log_sum = [t.data for t in rows_out.unbind(0)]
     top_ids = top_logprobs = None
     if top_k > 0:
         top_ids = empty(lead + (top_k,), dtype=torch.int64, device=device)

@@ -208,3 +208,24 @@ def test_a_second_derivative_is_refused():
         g, = torch.autograd.grad(f().square().sum(), u, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             g.sum().backward()
+
+
+def test_results_can_be_changed_in_place():
+    """A loss masked in place, as training loops do: each result is a tensor of its own for autograd."""
+    import torch
+    from paper_2608_02032_amd import layer
+    torch.manual_seed(4)
+    l = torch.randn(6, 300, device="cuda", requires_grad=True)
+    t = torch.arange(6, device="cuda") * 40
+    wt = torch.rand(6, device="cuda")
+    lp, ent = layer.token_logprobs(l, t)
+    want, = torch.autograd.grad((lp * wt).sum() - 0.1 * ent.sum(), l)
+    lp, ent = layer.token_logprobs(l, t)
+    lp *= wt
+    (lp.sum() - 0.1 * ent.sum()).backward()
+    assert l.grad.equal(want)
+    # what the backward needs of a result is still guarded
+    lp, ent = layer.token_logprobs(l, t)
+    ent *= 2
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        ent.sum().backward()
