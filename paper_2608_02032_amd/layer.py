@@ -173,7 +173,8 @@ class _TokenLogprobs(torch.autograd.Function):
 
 def add_norm(u, d, w):
     """(u + d, RMSNorm(u + d) w), differentiable: the residual addition with the
-    norm that follows it (dart.layernorm)."""
+    norm that follows it (dart.layernorm: both of one type, float32 or bfloat16, and
+    one shape, at most 16384 channels)."""
     return _AddNorm.apply(u, d, w)
 
 
@@ -187,6 +188,16 @@ def token_logprobs(logits, targets, ignore_index=-100):
 # --------------------------------------------------------------------------- #
 # the block and a small language model
 # --------------------------------------------------------------------------- #
+
+_NORM_DIM = 16384   # the widest row of dart.layernorm
+
+
+def _rmsnorm(u, w, eps=dart.DEFAULT_EPS):
+    """RMSNorm(u) w in the library's kernel; a residual stream of another type than
+    the float32 weights, or of wider rows, in elementwise torch ops."""
+    if u.is_cuda and u.dtype == w.dtype == torch.float32 and u.shape[-1] <= _NORM_DIM:
+        return _Norm.apply(u, w)
+    return u * torch.rsqrt(u.pow(2).mean(-1, keepdim=True) + eps) * w
 
 
 class DartBlock(nn.Module):
@@ -223,7 +234,7 @@ class DartBlock(nn.Module):
     def forward(self, u):
         B_, L, _ = u.shape
         H, P, N, G = self.H, self.P, self.N, self.G
-        proj = self.in_proj(_Norm.apply(u, self.norm_w))
+        proj = self.in_proj(_rmsnorm(u, self.norm_w))
         z, xbc, dtr, q, e, g = torch.split(proj, self.splits, dim=-1)
         xbc = _ConvSiLU.apply(xbc.contiguous(), self.conv_w, self.conv_b)
         x, Bm, Cm = torch.split(xbc, [self.d_inner, G * N, G * N], dim=-1)
@@ -255,7 +266,7 @@ class DartLM(nn.Module):
         u = self.emb(tokens)
         for blk in self.blocks:
             u = blk(u)
-        return self.head(_Norm.apply(u, self.norm_w))
+        return self.head(_rmsnorm(u, self.norm_w))
 
 
 def train_mqar(steps, L=256, R=None, batch=64, d_model=64, d_state=16, chunk=16, lr=1e-3,

@@ -229,3 +229,31 @@ def test_results_can_be_changed_in_place():
     ent *= 2
     with pytest.raises(RuntimeError, match="modified by an inplace"):
         ent.sum().backward()
+
+
+def test_residual_streams_that_the_norm_kernel_does_not_take():
+    """A bfloat16 residual stream under float32 weights (promoted by the norm) and rows of more than 16384 channels."""
+    import torch
+    from paper_2608_02032_amd import layer
+    torch.manual_seed(7)
+    blk = layer.DartBlock(64, 16, 64, 2, 16).cuda()
+    u = torch.randn(2, 48, 64, device="cuda").to(torch.bfloat16).requires_grad_()
+    y = blk(u)
+    assert y.dtype == torch.float32
+    y.square().mean().backward()
+    # the same stream in float32: the norm's bfloat16 roundings (the square, its mean, the reciprocal root, the product,
+    # half a step 2^-8 each), times a block's gain, at most eight: every branch ends in a norm
+    v = u.detach().float().requires_grad_()
+    z = blk(v)
+    z.square().mean().backward()
+    near(y, z, rel=8 * 4 * 2.0 ** -8, what="bf16 stream")
+    assert u.grad.dtype == torch.bfloat16 and bool(torch.isfinite(u.grad).all())
+    D = 16384 + 64
+    lm = layer.DartLM(24, D, n_layers=0).cuda()
+    tok = torch.randint(0, 24, (2, 5), device="cuda")
+    logits = lm(tok)
+    logits.square().sum().backward()
+    e = lm.emb.weight.detach().double()[tok]
+    want = (e * torch.rsqrt(e.square().mean(-1, keepdim=True) + 1e-6)) @ lm.head.weight.detach().double().t()
+    near(logits, want, rel=1e-4, what="wide")   # products of 16448 terms: sqrt of it, 128, half steps
+    assert bool(lm.norm_w.grad.any())
