@@ -517,3 +517,20 @@ def test_alternatives_of_rows_of_one_wave(dtype, V):
         assert dart.token_logprobs(l, top_k=k)["top_ids"].equal(order[:, :k]), k
         one = dart.token_logprobs_grad(l, torch.zeros(len(a), dtype=torch.int64, device="cuda"), torch.ones(len(a), device="cuda"), top_k=k)
         assert one["top_ids"].equal(order[:, :k]), k
+
+
+@pytest.mark.parametrize("dtype,V,R", [("fp32", (1 << 24) - 4095, 1), ("bf16", 1 << 24, 1), ("bf16", 4096 * 255 + 1, 2), ("fp32", 2048 * 200 + 3, 3)])
+def test_gradients_of_many_segments(dtype, V, R):
+    """Every element of the gradient that follows the segments' joining, target and weights included."""
+    import torch
+    print("\n[gpu-case] logprobs gradient of many segments %s V=%d R=%d" % (dtype, V, R), flush=True)
+    rng = np.random.default_rng(V + 1)
+    l = tensor(rng.standard_normal((R, V), dtype=np.float32) * 2, dtype)
+    t = np.array([V - 1, 0, V // 2])[:R]
+    ref = reference(f64(l), t, 0)
+    dlp, dent = tensor(rng.standard_normal(R)), tensor(rng.standard_normal(R))
+    for gdtype in {"fp32", dtype}:
+        gt = torch.bfloat16 if gdtype == "bf16" else torch.float32
+        for use in ((dlp, None), (dlp, dent)):
+            one = dart.token_logprobs_grad(l, ids(t), use[0], dentropy=use[1], grad_dtype=gt)["dlogits"]
+            check_grad(ref, t, use[0], use[1], None, one, gdtype)
