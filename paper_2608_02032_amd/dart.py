@@ -721,9 +721,14 @@ def _token_logprobs(logits, targets, top_k, ignore_index, stream, grad=None):
         for k in ("dlogprob", "dentropy", "dlse"):
             _same(grad[k], lead, torch.float32, k)
     empty = _allocator(stream)
-    rows_out = empty((4,) + lead, dtype=torch.float32, device=device)
-    # (.data: each a tensor of its own to autograd, which would take a change of one in place for a change of all)
-    logprob, entropy, row_max, log_sum = [t.data for t in rows_out.unbind(0)]
+    # one allocation, but each a tensor of its own to autograd, which would take a change of one view in place for
+    # a change of all
+    if lead:
+        rows_out = empty((4 * lead[0],) + lead[1:], dtype=torch.float32, device=device)
+        logprob, entropy, row_max, log_sum = rows_out.unsafe_split_with_sizes((lead[0],) * 4)
+    else:
+        rows_out = empty((4,), dtype=torch.float32, device=device)
+        logprob, entropy, row_max, log_sum = [t.data for t in rows_out.unbind(0)]
     top_ids = top_logprobs = None
     if top_k > 0:
         top_ids = empty(lead + (top_k,), dtype=torch.int64, device=device)

@@ -229,6 +229,13 @@ def test_results_can_be_changed_in_place():
     ent *= 2
     with pytest.raises(RuntimeError, match="modified by an inplace"):
         ent.sum().backward()
+    # whatever the leading axes, none of them too
+    for shape in ((300,), (2, 3, 300), (0, 300), (4, 0, 300)):
+        l = torch.randn(shape, device="cuda", requires_grad=True)
+        lp, ent = layer.token_logprobs(l, torch.zeros(shape[:-1], dtype=torch.int64, device="cuda"))
+        lp *= 0.5
+        (lp.sum() + ent.sum()).backward()
+        assert lp.shape == ent.shape == shape[:-1] and l.grad.shape == shape
 
 
 def test_residual_streams_that_the_norm_kernel_does_not_take():
