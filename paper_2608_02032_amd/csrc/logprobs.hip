@@ -18,8 +18,9 @@
 // are cut into segments, one per workgroup, whose results a second launch joins.
 // 16384 rows of 50257 bf16: forward 287 us (5.7 TB/s), the gradient after it 556 us
 // (5.9 TB/s), both in one pass 680 us (4.8 TB/s, as a copy); with five alternatives
-// 8192 rows take 213 us instead of 147; 4096 rows of 131072 forward 180 us (6.0 TB/s);
-// one row of 131072 with twenty alternatives 10 us and 8 us for the join.
+// 8192 rows take 213 us instead of 147; 4096 rows of 131072 forward 180 us (6.0 TB/s),
+// with the gradient, a row in 1024 threads, 469 us (4.6 TB/s; 8192 of 50257 float 700,
+// 4.7 TB/s); one row of 131072 with twenty alternatives 10 us and 8 us for the join.
 #include "dart_common.hpp"
 #include "dart_internal.hpp"
 
@@ -412,11 +413,12 @@ __device__ __forceinline__ void put_steep(const Cut<T, align_for(TPR)>& cut, GT*
 
 // Waves a SIMD is to hold (by the registers of NV packed vectors), and with them
 // the workgroups of a CU: the grid of the whole-row kernels.  More of them hide the
-// sums of one row behind the loads of others, as far as the registers go without
-// spills in the loops (16384 rows of 50257 bf16, 13 vectors: six 284 us, four 306;
-// 65536 of 10000, 8 vectors: eight 332, five 359; with five alternatives and 4
-// vectors, 33554 rows of 4000 float: eight 120, seven 147; but with one and 13
-// vectors six, which spill, 401 and four 372).
+// sums of one row behind the loads of others (16384 rows of 50257 bf16, 13 vectors: six
+// 284 us, four 306; 65536 of 10000, 8 vectors: eight 332, five 359; with five
+// alternatives and 4 vectors, 33554 rows of 4000 float: eight 120, seven 147; but with
+// one and 13 vectors six, which spill, 401 and four 372).  At these the forward's whole
+// rows spill nothing; with the gradient 2 registers of 8 vectors, 4 of 13 and 21 to 32
+// of 16 are spilt, with alternatives as well 2 to 10 up to two vectors, 14 to 22 of 8 and 13, 36 of 16.
 constexpr int waves_per_simd(int nv, bool grad, bool top) {
     return nv <= 2 || (!grad && nv <= (top ? 4 : 8)) ? 8 : nv <= 8 ? 5 : !grad && !top && nv <= 13 ? 6 : 4;
 }
@@ -768,6 +770,9 @@ struct Plan {
 };
 Plan plan_for(int64_t rows, int64_t vocab, int dtype, int top_k, bool grad) {
     const int vec = dtype == 1 ? 8 : 4;
+    // (13 vectors, between 8 and 16: the most that six waves hold forward, and with few
+    // spilt in the gradient; 12288 rows of 53248 bf16 in 13 and of 53256 in 16: forward
+    // 231 and 274 us, with five alternatives 328 and 385, with the gradient 541 and 582)
     static const int forms[][2] = {{64, 0}, {64, 1}, {64, 2}, {64, 4}, {256, 2}, {256, 4}, {256, 8}, {512, 8}, {512, 13}, {512, 16}, {1024, 16}};
     const int64_t most = 1024 * 16 * vec;
     // long rows without alternatives or gradient in segments of 256 threads, if those

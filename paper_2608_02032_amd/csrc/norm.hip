@@ -453,8 +453,9 @@ int64_t bwd_cap() { return (int64_t)device_cu_count() * 4; }
 // Float rows, with two vectors for one of bf16: up to 16 (100000 of 800, backward 182 and
 // 208, forward 119 and 131; 8192 of 2048 at 32 28.1 and 24.9).  Beyond that at most 16 per
 // lane.  Backward of more than 8192 columns, 16 elements in each of 1024
-// lanes: the column sums stand in LDS (4096 rows of 16384 bf16 with dsum 136 us, 4.0 TB/s; in
-// registers, spilt, 246).  Rows that are no multiple of a vector, at any alignment:
+// lanes: the column sums stand in LDS (4096 rows of 16384 bf16 with dsum 136 us, 4.0 TB/s, 8
+// registers still spilt; with the sums in registers 246), with float gradients at 46 registers
+// spilt (4096 of 16384 float with dsum 288 us, 3.7 TB/s; bf16 without dsum 220).  Rows that are no multiple of a vector, at any alignment:
 // 16384 rows of 4095 bf16 forward 5.0 TB/s, of 4096 6.7 (element by element 1.5).
 #define DART_NORM_FORMS(V, BWD, FEW, F)                 \
     if constexpr (V == 8) {                             \

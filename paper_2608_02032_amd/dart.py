@@ -839,7 +839,8 @@ def grad_norm(grads, scale=1.0, stream=None):
 
 def clip_grad_norm(grads, max_norm, scale=1.0, out=None, stream=None):
     """Scale the gradients by `scale` and by min(1, max_norm / (norm + 1e-6)),
-    norm being that of the scaled ones (dart_clip_grad_norm); in place, or into
+    norm being that of the scaled ones (dart_clip_grad_norm; an infinite max_norm
+    scales alone); in place, or into
     the tensors `out` of the same shapes, float32 or bfloat16 each.  Returns norm,
     a float32 tensor of no dimensions: nothing waits for the GPU.  Gradients and
     outputs are dense; no two outputs overlap."""
