@@ -392,7 +392,8 @@ dart_status dart_layernorm_bwd(int64_t rows, int32_t dim, int32_t dtype, int32_t
  *   by the lowest index (-0 equals 0; a NaN is above all).
  * A row whose target is ignore_index has logprob 0; any other target outside
  * [0, vocab) makes logprob NaN and reads nothing.  A logit of -infinity has
- * probability 0.  A row of nothing else has row_max = log_sum = -infinity,
+ * probability 0, and one below 2^-126 counts as 0 in the sums and the
+ * gradient.  A row of nothing but -infinity has row_max = log_sum = -infinity,
  * entropy 0 and, for every token, logprob -infinity.  A logit of NaN or
  * +infinity makes the row's log_sum, logprob and entropy NaN.
  *   logits   [rows][row_stride] storage dtype, any alignment; vocab <= 2^24
